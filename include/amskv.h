@@ -413,6 +413,70 @@ AMSKV_API int amskv_status(amskv_cache* cache, int* device_status);
  * amskv_status must then return AMSKV_ERR_DEVICE_TIMEOUT once, and AMSKV_OK afterwards. */
 AMSKV_API int amskv_selftest_wait_timeout(amskv_cache* cache, uint32_t iterations, void* stream);
 
+/*
+ * Rotary positions.  Channels 0 .. rotary_dim - 1 of a head are rotated in pairs, the others stay.  They fall into `axes` equal
+ * parts of P = rotary_dim / axes channels, one for each coordinate of a position (a raster token has two: row and column; a
+ * token number is one), and pair i of axis a turns by positions[a] * w_i, i < P / 2:
+ *   (u, v) -> amplitude * (u cos - v sin, v cos + u sin)
+ *   layout   AMSKV_ROTARY_HALF: channels a P + i and a P + i + P / 2;  AMSKV_ROTARY_INTERLEAVED: a P + 2 i and a P + 2 i + 1
+ *   scaling  AMSKV_ROTARY_PLAIN:   w_i = base^(-2 i / P)
+ *            AMSKV_ROTARY_LINEAR:  w_i / factor (positions interpolated)
+ *            AMSKV_ROTARY_BASE:    base * factor^(P / (P - 2)) in place of base (P > 2)
+ *            AMSKV_ROTARY_BY_PARTS: w_i (1 - g_i) + (w_i / factor) g_i, where g_i rises linearly from 0 at index lo to 1 at
+ *              index hi: the floor (ceiling) of P ln(original_length / (2 pi beta)) / (2 ln base) for beta_fast (beta_slow)
+ *              turns over the original length, clamped to [0, P - 1]; hi = lo + 0.001 where they coincide
+ *   amplitude  0 selects 1, and 1 + 0.1 ln(factor) for BY_PARTS with factor > 1
+ */
+#define AMSKV_ROTARY_HALF 0
+#define AMSKV_ROTARY_INTERLEAVED 1
+#define AMSKV_ROTARY_PLAIN 0
+#define AMSKV_ROTARY_LINEAR 1
+#define AMSKV_ROTARY_BASE 2
+#define AMSKV_ROTARY_BY_PARTS 3
+typedef struct {
+    int32_t rotary_dim;      /* even multiple of axes, at most 256                            */
+    int32_t axes;            /* 1 .. 3                                                        */
+    int32_t layout;
+    int32_t scaling;
+    double base;             /* > 1                                                           */
+    double factor;           /* >= 1; not used by PLAIN                                       */
+    double original_length;  /* BY_PARTS only, as are the two below: > 0                      */
+    double beta_fast;        /* > beta_slow                                                   */
+    double beta_slow;        /* > 0                                                           */
+    double amplitude;        /* >= 0                                                          */
+} amskv_rotary_spec;
+
+/* Bytes of a table of `count` positions: count * rotary_dim / 2 pairs (cos, sin) of floats. */
+AMSKV_API int amskv_rotary_table_bytes(const amskv_rotary_spec* spec, int64_t count, size_t* bytes);
+
+/*
+ * Fills a table: row n holds amplitude * (cos, sin) of the angles of position n, columns in axis-major order.  Made once for
+ * a schedule (its scales one behind the other, say); angles are formed in fp64.
+ *   positions   device pointer to count * axes floats, 4-byte aligned
+ *   table       device pointer, amskv_rotary_table_bytes() bytes, 16-byte aligned
+ * Enqueued on `stream`.  Errors: INVALID, CUDA.
+ */
+AMSKV_API int amskv_rotary_table(const amskv_rotary_spec* spec, const float* positions, int64_t count, float* table, void* stream);
+
+#define AMSKV_ROTARY_TRANSPOSED 1u /* flag of amskv_rotary: turns the other way.  The gradient of the rotation with respect to its
+                                      input, and its inverse where the amplitude is 1                                        */
+/*
+ * Rotates Q and K of a scale (what amskv_append and amskv_attend then take), in one launch.
+ *   Q, K, Q_out, K_out   device pointers, [rows, heads, T, head_dim] bf16, strides as in amskv_append; an output may be its input
+ *               (same pointer, same strides), and must not overlap anything else the call reads.  K = NULL with k_heads = 0: Q alone.
+ *               head_dim: a multiple of 8, rotary_dim .. 256.
+ *   table       of table_rows rows.  Token t takes row first + t (all of them inside the table), or
+ *   index       device pointer to int32: row index[r * index_row_stride + t] for token t of row r (index_row_stride 0: the same for
+ *               all rows); `first` is then not used.  A token whose index is outside the table has no position: its channels
+ *               are passed on as they are.
+ * Products and sums in fp32, one rounding to bf16.  Enqueued on `stream`.  Errors: INVALID, UNSUPPORTED (head_dim; more than 2^31 - 1
+ * tokens over all rows), CUDA.
+ */
+AMSKV_API int amskv_rotary(const amskv_rotary_spec* spec, const float* table, int64_t table_rows, int64_t first, const int32_t* index,
+                           int64_t index_row_stride, int rows, int T, int head_dim, int q_heads, const void* Q,
+                           const int64_t q_strides[3], void* Q_out, const int64_t q_out_strides[3], int k_heads, const void* K,
+                           const int64_t k_strides[3], void* K_out, const int64_t k_out_strides[3], uint32_t flags, void* stream);
+
 /* Number of kernels this library has launched since it was loaded. */
 AMSKV_API int64_t amskv_launch_count(void);
 

@@ -24,6 +24,9 @@ FLAG_BULK_APPEND = 2
 FLAG_TRANSIENT_LAST_SCALE = 4
 FLAG_NVTX = 8
 PATH_AUTO, PATH_SIMT, PATH_TENSOR, PATH_TENSOR_PAIR, PATH_SMALL = 0, 1, 2, 3, 4
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BY_PARTS = 0, 1, 2, 3
+ROTARY_TRANSPOSED = 1
 LAYER_EFFICIENT, LAYER_DEMANDING, LAYER_PROMOTABLE = 0, 1, 2
 
 
@@ -42,6 +45,12 @@ class Desc(ctypes.Structure):
                 ("scale_sides", ctypes.POINTER(ctypes.c_int32)), ("policy", ctypes.POINTER(LayerPolicy)),
                 ("softmax_scale", ctypes.c_float), ("flags", ctypes.c_uint32),
                 ("token_budget", ctypes.POINTER(TokenBudget))]
+
+
+class RotarySpec(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("axes", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double), ("original_length", ctypes.c_double),
+                ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double), ("amplitude", ctypes.c_double)]
 
 
 class AmskvError(RuntimeError):
@@ -76,6 +85,10 @@ def _load() -> ctypes.CDLL:
         "amskv_layer_similarity": ([vp, i, vp, i, i, i, i, vp, vp, sz, vp], i),
         "amskv_similarity_workspace_bytes": ([], sz),
         "amskv_layer_similarity_static": ([vp, i, vp, i, i, i, i, vp, vp], i),
+        "amskv_rotary_table_bytes": ([ctypes.POINTER(RotarySpec), ctypes.c_int64, szp], i),
+        "amskv_rotary_table": ([ctypes.POINTER(RotarySpec), vp, ctypes.c_int64, vp, vp], i),
+        "amskv_rotary": ([ctypes.POINTER(RotarySpec), vp, ctypes.c_int64, ctypes.c_int64, vp, ctypes.c_int64, i, i, i,
+                          i, vp, i64p, vp, i64p, i, vp, i64p, vp, i64p, ctypes.c_uint32, vp], i),
         "amskv_classify_by_threshold": ([dp, i, ctypes.c_double, i32p], i),
         "amskv_classify_lowest": ([dp, i, i, i32p], i),
         "amskv_kept_segments": ([vp, i, i, i32p, i32p], i),
@@ -103,7 +116,7 @@ except ImportError:   # not built for this interpreter: every call goes through 
     _steps = None
 EXPORTS = ("amskv_cache_required_bytes amskv_cache_create amskv_cache_destroy amskv_cache_reset amskv_append "
            "amskv_attend amskv_append_attend amskv_attention_density amskv_attend_density amskv_first_overflow_scale amskv_promote_layer amskv_set_attend_path amskv_step_host amskv_step_staging_bytes amskv_layer_similarity "
-           "amskv_similarity_workspace_bytes amskv_layer_similarity_static amskv_classify_by_threshold amskv_classify_lowest "
+           "amskv_similarity_workspace_bytes amskv_layer_similarity_static amskv_rotary_table_bytes amskv_rotary_table amskv_rotary amskv_classify_by_threshold amskv_classify_lowest "
            "amskv_kept_segments amskv_evicted_at amskv_resident_ranges amskv_attended_tokens amskv_append_copies "
            "amskv_cache_bytes amskv_status amskv_selftest_wait_timeout "
            "amskv_launch_count amskv_strerror").split()
@@ -291,6 +304,41 @@ def amskv_layer_similarity_static(K_prev, side_prev: int, K_cur, side_cur: int, 
     array, so they must not overlap on the GPU; problems above 2^30 16-byte chunks are refused."""
     _check(lib.amskv_layer_similarity_static(_addr(K_prev), side_prev, _addr(K_cur), side_cur, rows, heads, head_dim,
                                              _addr(out_ss), _stream(stream)), "amskv_layer_similarity_static")
+
+
+def make_rotary(rotary_dim: int, axes: int = 1, layout: int = ROTARY_HALF, base: float = 10000.0, scaling: int = ROTARY_PLAIN,
+                factor: float = 1.0, original_length: float = 0.0, beta_fast: float = 32.0, beta_slow: float = 1.0,
+                amplitude: float = 0.0) -> RotarySpec:
+    return RotarySpec(int(rotary_dim), int(axes), int(layout), int(scaling), float(base), float(factor), float(original_length),
+                      float(beta_fast), float(beta_slow), float(amplitude))
+
+
+def amskv_rotary_table_bytes(spec: RotarySpec, count: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.amskv_rotary_table_bytes(ctypes.byref(spec), int(count), ctypes.byref(n)), "amskv_rotary_table_bytes")
+    return int(n.value)
+
+
+def amskv_rotary_table(spec: RotarySpec, positions, count: int, table, stream=None) -> None:
+    """positions: device floats [count, axes]; table: device floats [count, rotary_dim / 2, 2]."""
+    _check(lib.amskv_rotary_table(ctypes.byref(spec), _addr(positions), int(count), _addr(table), _stream(stream)),
+           "amskv_rotary_table")
+
+
+def amskv_rotary(spec: RotarySpec, table, table_rows: int, first: int, index, rows: int, T: int, head_dim: int, q_heads: int, Q,
+                 Q_out, k_heads: int = 0, K=None, K_out=None, transposed: bool = False, stream=None, index_row_stride=None) -> None:
+    """Rotates Q (and K) by rows first .. first + T - 1 of the table, or by the rows `index` names: device int32 [T] or
+    [rows, T] (a tensor, or an address with index_row_stride)."""
+    if index_row_stride is None:
+        index_row_stride = 0
+        if hasattr(index, "stride"):
+            assert index.dim() in (1, 2) and (index.shape[-1] == 1 or index.stride(-1) == 1), "expected [T] or [rows, T], tokens contiguous"
+            index_row_stride = index.stride(0) if index.dim() == 2 else 0
+    for name, x in (("rows", rows), ("T", T), ("head_dim", head_dim), ("q_heads", q_heads), ("k_heads", k_heads)):
+        _int32(name, x)
+    _check(lib.amskv_rotary(ctypes.byref(spec), _addr(table), int(table_rows), int(first), _addr(index), int(index_row_stride), rows, T,
+                            head_dim, q_heads, _addr(Q), _strides(Q), _addr(Q_out), _strides(Q_out), k_heads, _addr(K), _strides(K),
+                            _addr(K_out), _strides(K_out), ROTARY_TRANSPOSED if transposed else 0, _stream(stream)), "amskv_rotary")
 
 
 def amskv_classify_by_threshold(scores: Sequence[float], theta: float) -> List[bool]:

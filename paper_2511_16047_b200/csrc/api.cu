@@ -180,6 +180,63 @@ int make_strided(const void* ptr, const int64_t* strides, int32_t rows, int32_t 
     return AMSKV_OK;
 }
 
+// SMs of the current device, for calls that no cache belongs to; 0 on failure
+int current_sm_count()
+{
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    return n;
+}
+
+bool good_rotary_spec(const amskv_rotary_spec* s)
+{
+    if (!s || s->axes < 1 || s->axes > 3 || s->rotary_dim < 2 || s->rotary_dim > kMaxRotaryDim || s->rotary_dim % (2 * s->axes)) return false;
+    if (s->layout != AMSKV_ROTARY_HALF && s->layout != AMSKV_ROTARY_INTERLEAVED) return false;
+    if (s->scaling < AMSKV_ROTARY_PLAIN || s->scaling > AMSKV_ROTARY_BY_PARTS) return false;
+    if (!(s->base > 1.0) || !std::isfinite(s->base) || !(s->amplitude >= 0.0) || !std::isfinite(s->amplitude)) return false;
+    if (s->scaling != AMSKV_ROTARY_PLAIN && (!(s->factor >= 1.0) || !std::isfinite(s->factor))) return false;
+    if (s->scaling == AMSKV_ROTARY_BASE && s->rotary_dim / s->axes <= 2) return false;
+    if (s->scaling == AMSKV_ROTARY_BY_PARTS &&
+        (!(s->original_length > 0.0) || !std::isfinite(s->original_length) || !(s->beta_slow > 0.0) || !(s->beta_fast > s->beta_slow) ||
+         !std::isfinite(s->beta_fast)))
+        return false;
+    return true;
+}
+
+RotaryFrequencies rotary_frequencies(const amskv_rotary_spec& s)
+{
+    constexpr double kPi = 3.14159265358979323846;
+    RotaryFrequencies f;
+    const int32_t P = s.rotary_dim / s.axes;
+    f.n = P / 2;
+    f.axes = s.axes;
+    double base = s.base, amplitude = s.amplitude;
+    if (s.scaling == AMSKV_ROTARY_BASE) base *= std::pow(s.factor, (double)P / (P - 2));
+    double lo = 0.0, hi = 0.0;
+    if (s.scaling == AMSKV_ROTARY_BY_PARTS) {
+        auto index_of = [&](double beta) { return P * std::log(s.original_length / (2.0 * kPi * beta)) / (2.0 * std::log(s.base)); };
+        lo = std::min(std::max(std::floor(index_of(s.beta_fast)), 0.0), P - 1.0);
+        hi = std::min(std::max(std::ceil(index_of(s.beta_slow)), 0.0), P - 1.0);
+        if (hi <= lo) hi = lo + 0.001;
+        if (amplitude == 0.0) amplitude = 1.0 + 0.1 * std::log(s.factor);
+    }
+    if (amplitude == 0.0) amplitude = 1.0;
+    f.amplitude = (float)amplitude;
+    for (int32_t i = 0; i < f.n; ++i) {
+        double w = std::pow(base, -2.0 * i / P);
+        if (s.scaling == AMSKV_ROTARY_LINEAR) w /= s.factor;
+        if (s.scaling == AMSKV_ROTARY_BY_PARTS) {
+            const double g = std::min(std::max((i - lo) / (hi - lo), 0.0), 1.0);
+            w = w * (1.0 - g) + w / s.factor * g;
+        }
+        f.half_turns[i] = w / kPi;
+    }
+    return f;
+}
+
 // host-side state after scale `scale` of `layer` was stored
 void note_appended(amskv_cache* cache, int layer, int scale)
 {
@@ -700,6 +757,68 @@ int amskv_step_host(amskv_cache* cache, int layer, int scale, const void* K_host
     int rc = amskv_append_attend(cache, layer, scale, s, s + one, nullptr, s + 2 * one, s + 3 * one, nullptr, nullptr, stream);
     if (rc != AMSKV_OK) return rc;
     e = cudaMemcpyAsync(out_host, s + 3 * one, bytes, cudaMemcpyDeviceToHost, st);
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
+    return AMSKV_OK;
+}
+
+int amskv_rotary_table_bytes(const amskv_rotary_spec* spec, int64_t count, size_t* bytes)
+{
+    if (!good_rotary_spec(spec) || !bytes || count < 1 || count > (1ll << 40)) return AMSKV_ERR_INVALID;
+    *bytes = (size_t)count * (size_t)(spec->rotary_dim / 2) * sizeof(float2);
+    return AMSKV_OK;
+}
+
+int amskv_rotary_table(const amskv_rotary_spec* spec, const float* positions, int64_t count, float* table, void* stream)
+{
+    if (!good_rotary_spec(spec) || !positions || !table || count < 1 || count > (1ll << 40)) return AMSKV_ERR_INVALID;
+    if (misaligned(table) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return AMSKV_ERR_INVALID;
+    const int sms = current_sm_count();
+    if (sms == 0) return AMSKV_ERR_CUDA;
+    const cudaError_t e = launch_rotary_table(positions, rotary_frequencies(*spec), count, reinterpret_cast<float2*>(table), sms,
+                                              static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
+    return AMSKV_OK;
+}
+
+int amskv_rotary(const amskv_rotary_spec* spec, const float* table, int64_t table_rows, int64_t first, const int32_t* index,
+                 int64_t index_row_stride, int rows, int T, int head_dim, int q_heads, const void* Q, const int64_t q_strides[3],
+                 void* Q_out, const int64_t q_out_strides[3], int k_heads, const void* K, const int64_t k_strides[3], void* K_out,
+                 const int64_t k_out_strides[3], uint32_t flags, void* stream)
+{
+    if (!good_rotary_spec(spec) || !table || misaligned(table) || table_rows < 1 || table_rows > (1ll << 40)) return AMSKV_ERR_INVALID;
+    if (rows < 1 || T < 1 || head_dim < spec->rotary_dim || q_heads < 1 || k_heads < 0 || (flags & ~AMSKV_ROTARY_TRANSPOSED)) return AMSKV_ERR_INVALID;
+    if (head_dim % 8 || head_dim > kMaxRotaryDim || (int64_t)rows * T > 0x7fffffffll) return AMSKV_ERR_UNSUPPORTED;
+    if (index ? (reinterpret_cast<uintptr_t>(index) & 3u) != 0 || index_row_stride < 0 : first < 0 || first > table_rows - T) return AMSKV_ERR_INVALID;
+    if (k_heads == 0 && (K || K_out)) return AMSKV_ERR_INVALID;
+    RotaryArgs a = {};
+    Strided in, to;
+    for (int i = 0; i < (k_heads > 0 ? 2 : 1); ++i) {
+        const int heads = i ? k_heads : q_heads;
+        int rc = make_strided(i ? K : Q, i ? k_strides : q_strides, rows, heads, T, head_dim, &in);
+        if (rc == AMSKV_OK) rc = make_strided(i ? K_out : Q_out, i ? k_out_strides : q_out_strides, rows, heads, T, head_dim, &to, true);
+        if (rc != AMSKV_OK) return rc;
+        if (in.ptr == to.ptr && (in.row != to.row || in.head != to.head || in.token != to.token)) return AMSKV_ERR_INVALID;
+        a.x[i] = static_cast<const __nv_bfloat16*>(in.ptr);
+        a.y[i] = static_cast<__nv_bfloat16*>(const_cast<void*>(to.ptr));
+        a.x_row[i] = in.row, a.x_head[i] = in.head, a.x_tok[i] = in.token;
+        a.y_row[i] = to.row, a.y_head[i] = to.head, a.y_tok[i] = to.token;
+        a.heads[i] = heads;
+    }
+    a.table = reinterpret_cast<const float2*>(table);
+    a.index = index;
+    a.index_row = index_row_stride;
+    a.table_rows = table_rows;
+    a.first = first;
+    a.rows = rows;
+    a.T = T;
+    a.D = head_dim;
+    a.rotary_dim = spec->rotary_dim;
+    a.axes = spec->axes;
+    a.interleaved = spec->layout == AMSKV_ROTARY_INTERLEAVED;
+    a.direction = (flags & AMSKV_ROTARY_TRANSPOSED) ? -1.f : 1.f;
+    const int sms = current_sm_count();
+    if (sms == 0) return AMSKV_ERR_CUDA;
+    const cudaError_t e = launch_rotary(a, sms, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
     return AMSKV_OK;
 }

@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cstdint>
 
@@ -152,6 +153,28 @@ cudaError_t launch_zero(double* p, size_t n, cudaStream_t stream);
 cudaError_t launch_density(const Strided& Q, const LayerRegion& region, const DensityPieces& pieces, int32_t T,
                            int32_t rows, int32_t heads, int32_t D, float softmax_scale, double* out, cudaStream_t stream);
 
+// Rotary positions (rotary.cu).  Frequencies of one axis, in half turns per unit of position; every axis has the same.
+constexpr int kMaxRotaryDim = 256;
+struct RotaryFrequencies {
+    double half_turns[kMaxRotaryDim / 2];
+    int32_t n, axes;
+    float amplitude;
+};
+struct RotaryArgs {   // two tensors (Q and K; heads of an absent one: 0), each read from x and written to y (which may be x)
+    const __nv_bfloat16* x[2];
+    __nv_bfloat16* y[2];
+    int64_t x_row[2], x_head[2], x_tok[2], y_row[2], y_head[2], y_tok[2];   // element strides
+    int32_t heads[2];
+    const float2* table;   // [table_rows][rotary_dim / 2]
+    const int32_t* index;  // table row of every token, or null: first + token
+    int64_t index_row, table_rows, first;
+    int32_t rows, T, D, rotary_dim, axes, interleaved;
+    float direction;       // 1, or -1: the transpose
+};
+cudaError_t launch_rotary_table(const float* positions, const RotaryFrequencies& freq, int64_t count, float2* table, int sm_count,
+                                cudaStream_t stream);
+cudaError_t launch_rotary(const RotaryArgs& args, int sm_count, cudaStream_t stream);
+
 // One warp whose bounded wait runs out after `limit` iterations (nothing ever arrives): records
 // kStatusSyncTimeout in *status and returns normally.
 cudaError_t launch_wait_gives_up(uint32_t limit, int* status, cudaStream_t stream);
@@ -230,6 +253,24 @@ __device__ __forceinline__ uint4 load_16B_once(const void* p)   // (data that no
 {
     uint4 v;
     asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float load_float(const float* p)
+{
+    float v;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float2 load_float2(const float2* p)
+{
+    float2 v;
+    asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ int32_t load_int(const int32_t* p)
+{
+    int32_t v;
+    asm volatile("ld.global.s32 %0, [%1];" : "=r"(v) : "l"(p));
     return v;
 }
 __device__ __forceinline__ double load_double(const double* p)

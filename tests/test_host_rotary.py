@@ -1,0 +1,86 @@
+"""Rotary positions without a GPU: what the calls refuse, and the oracle's own identities."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as ref
+from paper_2511_16047_b200 import binding as B
+
+A = 1 << 20   # an aligned address that nothing reads: every call here is refused before any launch
+
+
+def _refused(code, **change):
+    args = dict(spec=B.make_rotary(64), table=A, table_rows=16, first=0, index=None, rows=2, T=4, head_dim=64, q_heads=2, Q=A,
+                Q_out=2 * A, k_heads=2, K=3 * A, K_out=4 * A)
+    args.update(change)
+    with pytest.raises(B.AmskvError) as e:
+        B.amskv_rotary(**args)
+    assert e.value.code == code, (change, e.value)
+
+
+@pytest.mark.parametrize("spec", [
+    B.make_rotary(0), B.make_rotary(63), B.make_rotary(258), B.make_rotary(6, axes=2), B.make_rotary(64, axes=0),
+    B.make_rotary(64, axes=4), B.make_rotary(64, layout=2), B.make_rotary(64, scaling=4), B.make_rotary(64, base=1.0),
+    B.make_rotary(64, base=float("nan")), B.make_rotary(64, base=float("inf")), B.make_rotary(64, amplitude=-1.0),
+    B.make_rotary(64, scaling=B.ROTARY_LINEAR, factor=0.5), B.make_rotary(64, scaling=B.ROTARY_LINEAR, factor=float("nan")),
+    B.make_rotary(2, scaling=B.ROTARY_BASE, factor=2.0), B.make_rotary(64, scaling=B.ROTARY_BY_PARTS, factor=2.0),
+    B.make_rotary(64, scaling=B.ROTARY_BY_PARTS, factor=2.0, original_length=100.0, beta_fast=1.0, beta_slow=1.0),
+    B.make_rotary(64, scaling=B.ROTARY_BY_PARTS, factor=2.0, original_length=100.0, beta_slow=0.0)])
+def test_bad_specs_are_refused(spec):
+    with pytest.raises(B.AmskvError) as e:
+        B.amskv_rotary_table_bytes(spec, 4)
+    assert e.value.code == B.ERR_INVALID
+    with pytest.raises(B.AmskvError) as e:
+        B.amskv_rotary_table(spec, A, 4, A)
+    assert e.value.code == B.ERR_INVALID
+    _refused(B.ERR_INVALID, spec=spec)
+
+
+def test_bad_arguments_are_refused():
+    for change in (dict(table=None), dict(table=A + 8), dict(table_rows=0), dict(rows=0), dict(T=0), dict(q_heads=0), dict(k_heads=-1),
+                   dict(first=-1), dict(first=13), dict(Q=None), dict(Q=A + 2), dict(Q_out=None), dict(K_out=None), dict(K=None),
+                   dict(k_heads=0), dict(index=A + 2), dict(index=A, index_row_stride=-1), dict(head_dim=56)):
+        _refused(B.ERR_INVALID, **change)
+    for change in (dict(head_dim=68), dict(head_dim=264), dict(rows=1 << 20, T=1 << 11, table_rows=1 << 11)):
+        _refused(B.ERR_UNSUPPORTED, **change)
+    for positions, count, table in ((None, 4, A), (A, 4, None), (A + 2, 4, A), (A, 4, A + 4), (A, 0, A)):
+        with pytest.raises(B.AmskvError) as e:
+            B.amskv_rotary_table(B.make_rotary(64), positions, count, table)
+        assert e.value.code == B.ERR_INVALID
+    # strides: an output that aliases itself, an input written to itself with other strides
+    x = torch.zeros(2, 2, 4, 64, dtype=torch.bfloat16)
+    _refused(B.ERR_INVALID, Q=x, Q_out=x[:1].expand(2, 2, 4, 64))
+    y = torch.zeros(2, 4, 2, 64, dtype=torch.bfloat16)
+    _refused(B.ERR_INVALID, Q=y.transpose(1, 2), Q_out=y.data_ptr())
+    with pytest.raises(AssertionError):
+        B.amskv_rotary(B.make_rotary(64), A, 16, 0, torch.zeros(4, 2, dtype=torch.int32).t(), 2, 4, 64, 2, A, A)
+    with pytest.raises(OverflowError):
+        B.amskv_rotary(B.make_rotary(64), A, 16, 0, None, 1 << 40, 4, 64, 2, A, A)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="a device is there")
+def test_without_a_device_the_calls_fail():
+    _refused(B.ERR_CUDA)
+    with pytest.raises(B.AmskvError) as e:
+        B.amskv_rotary_table(B.make_rotary(64), A, 4, A)
+    assert e.value.code == B.ERR_CUDA
+
+
+def test_table_bytes():
+    assert B.amskv_rotary_table_bytes(B.make_rotary(48, axes=2), 7) == 7 * 24 * 8
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("axes", [1, 2, 3])
+def test_oracle_rotation_is_a_rotation_by_relative_positions(interleaved, axes):
+    """Products of two rotated vectors depend on the difference of their positions only; the transpose undoes the rotation."""
+    rng = np.random.default_rng(axes)
+    dim = 12 * axes
+    x, y = rng.standard_normal((2, 1, dim + 8))
+    p, d = rng.integers(0, 50, (1, axes)).astype(float), rng.integers(0, 50, (1, axes)).astype(float)
+    turn = lambda v, pos, **kw: ref.rotate(v, ref.rotary_angles(pos, dim), axes, interleaved, **kw)   # noqa: E731
+    a = (turn(x, p) * turn(y, p + d)).sum()
+    b = (turn(x, 0 * p) * turn(y, d)).sum()
+    assert abs(a - b) < 1e-9
+    assert np.abs(turn(turn(x, p), p, transposed=True) - x).max() < 1e-12
+    assert (turn(x, p)[..., dim:] == x[..., dim:]).all()
