@@ -175,6 +175,37 @@ cudaError_t launch_rotary_table(const float* positions, const RotaryFrequencies&
                                 cudaStream_t stream);
 cudaError_t launch_rotary(const RotaryArgs& args, int sm_count, cudaStream_t stream);
 
+// An encoder's keys and values (keys.cuh): [rows, key/value heads, keys, D] with a length for every row, or, with offsets, all rows'
+// keys one behind the other in [key/value heads, keys, D].
+struct EncoderKeys {
+    const __nv_bfloat16 *K, *V;
+    int64_t row, head, tok;      // element strides, the same for K and V
+    const int32_t *lengths, *offsets;
+    int32_t keys, max_keys;      // extent of the tensor; the most that a row has
+};
+// A layer's region held in 8 bits: item i owns 2 * capacity * D codes, keys first, and 2 * capacity / 16 powers of two.
+struct HeldRegion {
+    uint8_t* codes;
+    int8_t* exps;
+    int32_t capacity;            // tokens per item, a multiple of 16
+};
+struct HeldKeys {
+    const uint8_t* codes;
+    const int8_t* exps;
+    int32_t capacity, blocks;    // blocks of 16 slots that the ranges cover
+    RangeList ranges;            // each starts on a block
+};
+cudaError_t launch_append_held(const Strided& K, const Strided& V, const HeldRegion& region, int32_t offset, int32_t T, int32_t rows,
+                               int32_t heads, int32_t D, int sm_count, cudaStream_t stream);
+// Positions offset .. offset + T - 1 of a layer's region (of bf16 values: exps null) to [rows, heads, T, D] tensors; K's strides hold for V.
+cudaError_t launch_read_segment(const void* region, const int8_t* exps, int32_t capacity, int32_t offset, int32_t T, int32_t rows,
+                                int32_t heads, int32_t D, const Strided& K, const Strided& V, int sm_count, cudaStream_t stream);
+// Warp-matrix kernel over either (attend_rows.cu); `group` query heads share a key/value head.
+cudaError_t launch_attend_rows(const Strided& Q, const Strided& O, const EncoderKeys& enc, int32_t T, int32_t rows, int32_t kv_heads,
+                               int32_t group, int32_t D, float softmax_scale, int sm_count, cudaStream_t stream);
+cudaError_t launch_attend_rows(const Strided& Q, const Strided& O, const HeldKeys& held, int32_t T, int32_t rows, int32_t heads,
+                               int32_t D, float softmax_scale, int sm_count, cudaStream_t stream);
+
 // One warp whose bounded wait runs out after `limit` iterations (nothing ever arrives): records
 // kStatusSyncTimeout in *status and returns normally.
 cudaError_t launch_wait_gives_up(uint32_t limit, int* status, cudaStream_t stream);
@@ -265,6 +296,12 @@ __device__ __forceinline__ float2 load_float2(const float2* p)
 {
     float2 v;
     asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float4 load_float4(const void* p)
+{
+    float4 v;
+    asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
     return v;
 }
 __device__ __forceinline__ int32_t load_int(const int32_t* p)

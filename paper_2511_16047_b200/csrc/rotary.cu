@@ -15,6 +15,8 @@ constexpr int kThreads = 256;
 // Entry (n, column) = (cos, sin) of positions[n][axis] * frequency, times the amplitude.  The angle is formed and reduced in 64 bits,
 // in half turns (the host divides the frequencies by pi): at position 10^6 an fp32 angle would be off by 0.06.  What is left,
 // within a quarter turn either way, is rounded to fp32 once (an angle error of 2^-26 pi) and goes through sincospif.
+// Four rows of a thread at a time: with one, the loop waits for its position.  131 071 x 64: 27.4 -> TABLE us.
+constexpr int kTableRows = 4;
 __global__ void __launch_bounds__(kThreads)
 rotary_table_kernel(const float* positions, const __grid_constant__ RotaryFrequencies freq, int64_t count, float2* table)
 {
@@ -24,17 +26,121 @@ rotary_table_kernel(const float* positions, const __grid_constant__ RotaryFreque
     if (row0 >= per_pass) return;
     const int32_t axis = col / freq.n;
     const double half_turns = freq.half_turns[col - axis * freq.n];
-    for (int64_t row = (int64_t)blockIdx.x * per_pass + row0; row < count; row += (int64_t)gridDim.x * per_pass) {
-        const double t = (double)load_float(positions + row * freq.axes + axis) * half_turns;
-        const double f = fma(-2.0, rint(0.5 * t), t), n = rint(f);   // f in [-1, 1]
-        float s, c;
-        sincospif((float)(f - n), &s, &c);
-        const float a = n != 0.0 ? -freq.amplitude : freq.amplitude;
-        table[row * cols + col] = make_float2(c * a, s * a);
+    const int64_t step = (int64_t)gridDim.x * per_pass;
+    for (int64_t row = (int64_t)blockIdx.x * per_pass + row0; row < count; row += kTableRows * step) {
+        float pos[kTableRows];
+#pragma unroll
+        for (int i = 0; i < kTableRows; ++i) pos[i] = row + i * step < count ? load_float(positions + (row + i * step) * freq.axes + axis) : 0.f;
+#pragma unroll
+        for (int i = 0; i < kTableRows; ++i) {
+            if (row + i * step >= count) break;
+            const double t = (double)pos[i] * half_turns;
+            const double f = fma(-2.0, rint(0.5 * t), t), n = rint(f);   // f in [-1, 1]
+            float s, c;
+            sincospif((float)(f - n), &s, &c);
+            const float a = n != 0.0 ? -freq.amplitude : freq.amplitude;
+            table[(row + i * step) * cols + col] = make_float2(c * a, s * a);
+        }
     }
 }
 
 // ---------------------------------------------------------------- the rotation
+// A thread turns two 16-byte pieces of the same token in kHeads heads, which share its 64 bytes of the table.  Half layout: a piece
+// and its partner, half a part away (P a multiple of 16); interleaved: pieces u and u + units, each complete in itself (rotary_dim a
+// multiple of 8).  What is not rotated is copied, two pieces a thread, unless the output is the input.
+template <bool kInterleaved, int kHeads>
+__global__ void __launch_bounds__(kThreads)
+rotary_kernel(const __grid_constant__ RotaryArgs a, int32_t units)
+{
+    const uint32_t at = blockIdx.x * (uint32_t)kThreads + threadIdx.x, rt = at / (uint32_t)units;
+    const int32_t unit = (int32_t)(at - rt * (uint32_t)units);
+    const int64_t row = rt / (uint32_t)a.T;
+    const int32_t t = (int32_t)(rt - (uint32_t)row * (uint32_t)a.T);
+    if (row >= a.rows) return;
+    const int32_t chunks = a.D / 8, cols = a.rotary_dim / 2;
+    int32_t first, second, col_first, col_second;   // pieces (second may be behind the head's end), and their columns
+    bool turn_first, turn_second;
+    if (kInterleaved) {
+        first = unit, second = unit + units;
+        turn_first = first * 8 < a.rotary_dim, turn_second = second * 8 < a.rotary_dim;
+        col_first = first * 4, col_second = second * 4;
+    } else {
+        const int32_t part = a.rotary_dim / a.axes / 16, pairs = part * a.axes;   // pieces in half a part; in half of all
+        turn_first = turn_second = unit < pairs;
+        const int32_t axis = unit / part, j = unit - axis * part, rest = 2 * pairs + 2 * (unit - pairs);
+        first = turn_first ? axis * 2 * part + j : rest;
+        second = turn_first ? first + part : rest + 1;
+        col_first = unit * 8, col_second = col_first + 4;
+    }
+    overlap_with_previous();
+    float4 cs[4];   // (cos, sin) of two pairs each
+#pragma unroll
+    for (int i = 0; i < 4; ++i) cs[i] = make_float4(1.f, 0.f, 1.f, 0.f);
+    const int64_t n = a.index ? (int64_t)load_int(a.index + row * a.index_row + t) : a.first + t;
+    if (n >= 0 && n < a.table_rows) {   // (a token without a position keeps its channels)
+        const float2* e = a.table + n * cols;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < 2 ? turn_first : turn_second)
+                cs[i] = load_float4(e + (i < 2 ? col_first : col_second) + 2 * (i & 1));
+    }
+    const int32_t head0 = blockIdx.y * kHeads;
+    uint4 x[kHeads][2];
+    __nv_bfloat16* dst[kHeads];
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+        int32_t head = head0 + h;
+        dst[h] = nullptr;
+        const int which = head >= a.heads[0];
+        if (which) head -= a.heads[0];
+        if (head >= a.heads[which]) continue;
+        const __nv_bfloat16* src = a.x[which] + row * a.x_row[which] + head * a.x_head[which] + t * a.x_tok[which];
+        dst[h] = a.y[which] + row * a.y_row[which] + head * a.y_head[which] + t * a.y_tok[which];
+        x[h][0] = load_16B(src + first * 8);
+        if (second < chunks) x[h][1] = load_16B(src + second * 8);
+    }
+    auto turn = [&](uint32_t& u, uint32_t& w, const float4& v) {   // the pairs (u.lo, w.lo) and (u.hi, w.hi)
+        const float u0 = __uint_as_float(u << 16), u1 = __uint_as_float(u & 0xffff0000u);
+        const float w0 = __uint_as_float(w << 16), w1 = __uint_as_float(w & 0xffff0000u);
+        const float s0 = a.direction * v.y, s1 = a.direction * v.w;
+        const __nv_bfloat162 nu = __floats2bfloat162_rn(fmaf(u0, v.x, -(w0 * s0)), fmaf(u1, v.z, -(w1 * s1)));
+        const __nv_bfloat162 nw = __floats2bfloat162_rn(fmaf(w0, v.x, u0 * s0), fmaf(w1, v.z, u1 * s1));
+        u = *reinterpret_cast<const uint32_t*>(&nu);
+        w = *reinterpret_cast<const uint32_t*>(&nw);
+    };
+    auto turn_inside = [&](uint32_t& p, const float c, const float sin) {   // the pair (p.lo, p.hi)
+        const float u = __uint_as_float(p << 16), w = __uint_as_float(p & 0xffff0000u), s = a.direction * sin;
+        const __nv_bfloat162 r = __floats2bfloat162_rn(fmaf(u, c, -(w * s)), fmaf(w, c, u * s));
+        p = *reinterpret_cast<const uint32_t*>(&r);
+    };
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+        if (!dst[h]) continue;
+        uint4 &u = x[h][0], &w = x[h][1];
+        if (kInterleaved) {
+            if (turn_first) {
+                turn_inside(u.x, cs[0].x, cs[0].y);
+                turn_inside(u.y, cs[0].z, cs[0].w);
+                turn_inside(u.z, cs[1].x, cs[1].y);
+                turn_inside(u.w, cs[1].z, cs[1].w);
+            }
+            if (turn_second) {
+                turn_inside(w.x, cs[2].x, cs[2].y);
+                turn_inside(w.y, cs[2].z, cs[2].w);
+                turn_inside(w.z, cs[3].x, cs[3].y);
+                turn_inside(w.w, cs[3].z, cs[3].w);
+            }
+        } else if (turn_first) {
+            turn(u.x, w.x, cs[0]);
+            turn(u.y, w.y, cs[1]);
+            turn(u.z, w.z, cs[2]);
+            turn(u.w, w.w, cs[3]);
+        }
+        *reinterpret_cast<uint4*>(dst[h] + first * 8) = u;
+        if (second < chunks) *reinterpret_cast<uint4*>(dst[h] + second * 8) = w;
+    }
+}
+
 // Any shape: tokens go through shared memory, so that a thread, which writes eight channels, finds their partners wherever they are.
 // Everything a block writes it has read before, so that the output may be the input.
 __global__ void __launch_bounds__(kThreads)
@@ -110,8 +216,23 @@ cudaError_t launch_rotary_table(const float* positions, const RotaryFrequencies&
 
 cudaError_t launch_rotary(const RotaryArgs& a, int sm_count, cudaStream_t stream)
 {
+    const int32_t heads = a.heads[0] + a.heads[1], P = a.rotary_dim / a.axes;
+    const bool in_place = a.x[0] == a.y[0] && (a.heads[1] == 0 || a.x[1] == a.y[1]);
+    if (a.interleaved ? a.rotary_dim % 8 == 0 : P % 16 == 0) {
+        const int32_t moved = in_place ? a.rotary_dim / 8 : a.D / 8, units = (moved + 1) / 2;   // pieces, two a thread
+        const int64_t threads = (int64_t)a.rows * a.T * units, blocks = (threads + kThreads - 1) / kThreads;
+        // Four heads a thread share their part of the table; one, where that would leave SMs with less than half of their threads.
+        const bool four = threads * ((heads + 3) / 4) >= 1024ll * sm_count;
+        const int32_t groups = four ? (heads + 3) / 4 : heads;
+        if (threads <= 0xffffffffll - kThreads && groups <= 65535) {
+            const dim3 grid((unsigned)blocks, (unsigned)groups);
+            auto* kernel = a.interleaved ? (four ? rotary_kernel<true, 4> : rotary_kernel<true, 1>)
+                                         : (four ? rotary_kernel<false, 4> : rotary_kernel<false, 1>);
+            return launch_kernel(true, kernel, grid, dim3(kThreads), KernelMemory(0), stream, a, units);
+        }
+    }
     const int32_t per_pass = kThreads / (a.D / 8);
-    const int64_t total = (int64_t)a.rows * (a.heads[0] + a.heads[1]) * a.T;
+    const int64_t total = (int64_t)a.rows * heads * a.T;
     const int64_t blocks = std::min<int64_t>((total + per_pass - 1) / per_pass, 8ll * sm_count);
     return launch_kernel(true, rotary_any_kernel, dim3((unsigned)blocks), dim3(kThreads), KernelMemory((size_t)kThreads * 16), stream, a);
 }
