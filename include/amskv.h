@@ -84,6 +84,19 @@ extern "C" {
                               named after the call, layer and scale (timeline tools show which kernels belong to
                               which step); no effect on results */
 
+#define AMSKV_FLAG_KV_E4M3 16u /* The cache holds K and V in 8 bits: e4m3 codes with a power of two for every block of 16 tokens of
+                              a (row, head) (K and V apart; the tokens of a scale, its last block possibly shorter), half the memory
+                              and half the bytes that attention reads.  The power is the least 2^e, e >= -100, with no |x| of the
+                              block above 448 * 2^e (1 for a block of zeros); a code is x * 2^-e rounded to nearest, ties to even;
+                              the value it stands for, code * 2^e, is exact in bf16, and attention is exact over these values
+                              as it is over those of a bf16 cache.  A value comes back within 2^-4 of itself (half a step), or
+                              2^-10 * 2^e where it is below 2^-6 * 2^e.  |x| must be below 2^127.
+                              Every scale starts on a block of its own, so that the arena rounds its room up to 16 tokens.
+                              amskv_append_attend makes the two calls it stands for; the densities (amskv_attention_density,
+                              amskv_attend_density) and AMSKV_PATH_SIMT are refused with UNSUPPORTED, and so are, at creation,
+                              token budgets (they cut scales inside a block), BULK_APPEND and TRANSIENT_LAST_SCALE.
+                              amskv_cache_bytes counts the codes of resident tokens, not the powers of two. */
+
 /* amskv_set_attend_path */
 #define AMSKV_PATH_AUTO 0   /* warp-per-item kernel for the coarse scales (at most 16 queries and 32
                                retained keys; CUDA-core kernel for a single query token with several
@@ -274,6 +287,41 @@ AMSKV_API int amskv_attention_density(amskv_cache* cache, int layer, int scale, 
 AMSKV_API int amskv_attend_density(amskv_cache* cache, int layer, int scale, const void* Q, void* out,
                                    const int64_t q_strides[3], const int64_t o_strides[3], double* density,
                                    size_t density_entries, void* stream);
+
+/*
+ * Copies a segment that `layer` retains now out of the cache, as bf16 (from a cache of 8 bits: the values its codes stand for).
+ *   K, V   device pointers, [rows, heads, T, head_dim]; strides as in amskv_append.
+ * Errors: ORDER (nothing appended, or the segment is not retained), UNSUPPORTED (a layer with a token budget), INVALID, CUDA.
+ */
+AMSKV_API int amskv_read_segment(amskv_cache* cache, int layer, int segment, void* K, void* V, const int64_t strides[3], void* stream);
+
+/*
+ * Cross attention: the queries of `scale` attend to an encoder's states (a text prompt's, say) instead of the cache, each row to
+ * its own:  out = softmax(softmax_scale * Q K^T) V.  The cache gives rows, heads, head_dim, the scale's tokens, softmax_scale and
+ * the path; nothing in it is read or changed, and there is no order contract.
+ *   K, V      device pointers: [rows, kv_heads, keys, head_dim], of which row r has the first lengths[r]; or, with offsets, the
+ *             keys of all rows one behind the other, [kv_heads, keys, head_dim], row r's from offsets[r] to offsets[r + 1] - 1.
+ *             Strides (row, head, token) as in amskv_append, but that a row stride of 0 gives all rows the same keys; the
+ *             row stride is not used with offsets.  A row's keys behind its last one are not read.
+ *   lengths   device pointer to rows int32, or NULL: all keys.
+ *   offsets   device pointer to rows + 1 int32, or NULL.  (Lengths and offsets that point outside the tensor are cut to it.)
+ *   max_keys  the most keys that a row has (0: `keys`); rows with more are cut to it.  It decides launch shapes: give the batch's
+ *             longest length where offsets are used.
+ *   kv_heads  divides heads: query head h reads key/value head h / (heads / kv_heads).
+ *   Q, out    as for amskv_attend.  out must not overlap any input.  A row without keys gets zeros.
+ * Path: AMSKV_PATH_SMALL and AMSKV_PATH_SIMT are the warp-matrix kernel, AMSKV_PATH_TENSOR and AMSKV_PATH_TENSOR_PAIR the tensor-memory
+ * kernel.  Arithmetic as for amskv_attend.  Enqueued on `stream`.  Errors: INVALID, UNSUPPORTED (plan-only; keys above 2^30), CUDA.
+ */
+typedef struct {
+    int32_t kv_heads;
+    int32_t keys;
+    int32_t max_keys;
+    const int32_t* lengths;
+    const int32_t* offsets;
+} amskv_encoder;
+AMSKV_API int amskv_cross_attend(amskv_cache* cache, int scale, const amskv_encoder* encoder, const void* K, const void* V,
+                                 const int64_t kv_strides[3], const void* Q, void* out, const int64_t q_strides[3],
+                                 const int64_t o_strides[3], void* stream);
 
 /*
  * On-line promotion (Sec. 4.3, Algorithm 1: when the cache first exceeds the budget C_min and the

@@ -52,3 +52,43 @@ def rotate(x, angles, axes, interleaved=False, amplitude=1.0, transposed=False):
     u, w = y[..., pairs[:, 0]], y[..., pairs[:, 1]]
     y[..., pairs[:, 0]], y[..., pairs[:, 1]] = u * c - w * s, w * c + u * s
     return y
+
+
+def held_exponents(x):
+    """Powers of two of the blocks of 16 tokens: x [..., T, D] -> [..., ceil(T / 16)] integers."""
+    T = x.shape[-2]
+    out = []
+    for b in range(0, T, 16):
+        top = np.abs(x[..., b:b + 16, :]).max((-2, -1))
+        e = np.zeros(top.shape, dtype=np.int64)
+        for i in np.ndindex(top.shape):
+            if top[i] > 0:
+                e[i] = -100
+                while top[i] > 448.0 * 2.0 ** e[i]:
+                    e[i] += 1
+        out.append(e)
+    return np.stack(out, -1)
+
+
+def round_e4m3(y):
+    """To the nearest number of 4 significant bits, in steps of 2^-9 below 2^-6; ties to even."""
+    size = np.maximum(np.abs(y), 2.0 ** -6)
+    step = np.exp2(np.floor(np.log2(size)) - 3)
+    step = np.where(size < step * 8, step / 2, np.where(size >= step * 16, step * 2, step))   # (log2 may be off by a rounding)
+    return np.round(y / step) * step
+
+
+def held_values(x):
+    """What a cache of 8 bits gives back for x [..., T, D]."""
+    e = np.repeat(held_exponents(x), 16, -1)[..., :x.shape[-2], None].astype(np.float64)
+    return round_e4m3(x * np.exp2(-e)) * np.exp2(e)
+
+
+def attention(q, k, v, scale):
+    """[..., T, D] over [..., S, D]: the outputs, and the same sums with |v| (what roundings of the probabilities are measured by)."""
+    if k.shape[-2] == 0:
+        return np.zeros(q.shape), np.zeros(q.shape)
+    s = scale * (q @ np.swapaxes(k, -1, -2))
+    p = np.exp(s - s.max(-1, keepdims=True))
+    p /= p.sum(-1, keepdims=True)
+    return p @ v, p @ np.abs(v)

@@ -23,6 +23,7 @@ FLAG_PLAN_ONLY = 1
 FLAG_BULK_APPEND = 2
 FLAG_TRANSIENT_LAST_SCALE = 4
 FLAG_NVTX = 8
+FLAG_KV_E4M3 = 16
 PATH_AUTO, PATH_SIMT, PATH_TENSOR, PATH_TENSOR_PAIR, PATH_SMALL = 0, 1, 2, 3, 4
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BY_PARTS = 0, 1, 2, 3
@@ -45,6 +46,11 @@ class Desc(ctypes.Structure):
                 ("scale_sides", ctypes.POINTER(ctypes.c_int32)), ("policy", ctypes.POINTER(LayerPolicy)),
                 ("softmax_scale", ctypes.c_float), ("flags", ctypes.c_uint32),
                 ("token_budget", ctypes.POINTER(TokenBudget))]
+
+
+class Encoder(ctypes.Structure):
+    _fields_ = [("kv_heads", ctypes.c_int32), ("keys", ctypes.c_int32), ("max_keys", ctypes.c_int32), ("lengths", ctypes.c_void_p),
+                ("offsets", ctypes.c_void_p)]
 
 
 class RotarySpec(ctypes.Structure):
@@ -77,6 +83,8 @@ def _load() -> ctypes.CDLL:
         "amskv_append_attend": ([vp, i, i, vp, vp, i64p, vp, vp, i64p, i64p, vp], i),
         "amskv_attention_density": ([vp, i, i, vp, i64p, vp, sz, vp], i),
         "amskv_attend_density": ([vp, i, i, vp, vp, i64p, i64p, vp, sz, vp], i),
+        "amskv_read_segment": ([vp, i, i, vp, vp, i64p, vp], i),
+        "amskv_cross_attend": ([vp, i, ctypes.POINTER(Encoder), vp, vp, i64p, vp, vp, i64p, i64p, vp], i),
         "amskv_set_attend_path": ([vp, i], i),
         "amskv_first_overflow_scale": ([vp, i, ctypes.POINTER(i)], i),
         "amskv_promote_layer": ([vp, i], i),
@@ -115,7 +123,7 @@ try:
 except ImportError:   # not built for this interpreter: every call goes through ctypes
     _steps = None
 EXPORTS = ("amskv_cache_required_bytes amskv_cache_create amskv_cache_destroy amskv_cache_reset amskv_append "
-           "amskv_attend amskv_append_attend amskv_attention_density amskv_attend_density amskv_first_overflow_scale amskv_promote_layer amskv_set_attend_path amskv_step_host amskv_step_staging_bytes amskv_layer_similarity "
+           "amskv_attend amskv_append_attend amskv_attention_density amskv_attend_density amskv_read_segment amskv_cross_attend amskv_first_overflow_scale amskv_promote_layer amskv_set_attend_path amskv_step_host amskv_step_staging_bytes amskv_layer_similarity "
            "amskv_similarity_workspace_bytes amskv_layer_similarity_static amskv_rotary_table_bytes amskv_rotary_table amskv_rotary amskv_classify_by_threshold amskv_classify_lowest "
            "amskv_kept_segments amskv_evicted_at amskv_resident_ranges amskv_attended_tokens amskv_append_copies "
            "amskv_cache_bytes amskv_status amskv_selftest_wait_timeout "
@@ -267,6 +275,23 @@ def amskv_attend_density(cache: int, layer: int, scale: int, Q, out, density, de
     """amskv_attend plus the attention density of the same queries, from one launch where the paired kernel serves."""
     _check(lib.amskv_attend_density(cache, layer, scale, _addr(Q), _addr(out), _strides(Q), _strides(out), _addr(density),
                                 int(density_entries), _stream(stream)), "amskv_attend_density")
+
+
+def amskv_read_segment(cache: int, layer: int, segment: int, K, V, stream=None) -> None:
+    """A retained segment as bf16, into K and V."""
+    _int32("layer", layer), _int32("segment", segment)
+    _check(lib.amskv_read_segment(cache, layer, segment, _addr(K), _addr(V), _kv_strides(K, V), _stream(stream)), "amskv_read_segment")
+
+
+def amskv_cross_attend(cache: int, scale: int, kv_heads: int, keys: int, K, V, Q, out, lengths=None, offsets=None, max_keys: int = 0,
+                       stream=None) -> None:
+    """The queries of `scale` over an encoder's states: K and V [rows, kv_heads, keys, D] with device int32 `lengths` [rows], or,
+    with device int32 `offsets` [rows + 1], [1, kv_heads, keys, D] (all rows one behind the other)."""
+    for name, x in (("scale", scale), ("kv_heads", kv_heads), ("keys", keys), ("max_keys", max_keys)):
+        _int32(name, x)
+    enc = Encoder(kv_heads, keys, max_keys, _addr(lengths), _addr(offsets))
+    _check(lib.amskv_cross_attend(cache, scale, ctypes.byref(enc), _addr(K), _addr(V), _kv_strides(K, V), _addr(Q), _addr(out), _strides(Q),
+                                  _strides(out), _stream(stream)), "amskv_cross_attend")
 
 
 def amskv_set_attend_path(cache: int, path: int) -> None:

@@ -10,7 +10,7 @@
 #include <nvtx3/nvToolsExt.h>   // header-only; ranges cost nothing measurable unless a profiler is attached
 
 #include "../../include/amskv.h"
-#include "kernels.cuh"
+#include "keys.cuh"
 
 namespace amskv {
 
@@ -52,10 +52,18 @@ struct amskv_cache {
     size_t resident_now = 0, peak = 0;
 
     bool plan_only() const { return (flags & AMSKV_FLAG_PLAN_ONLY) != 0; }
+    // K and V are held in 8 bits, a power of two for every 16 tokens of a (row, head)
+    bool held() const { return (flags & AMSKV_FLAG_KV_E4M3) != 0; }
     // the scale is the last one of a cache that never stores its last scale
     bool transient(int scale) const { return (flags & AMSKV_FLAG_TRANSIENT_LAST_SCALE) != 0 && scale == n_scales - 1; }
     int64_t items() const { return (int64_t)rows * heads; }
-    size_t token_bytes() const { return (size_t)items() * head_dim * 2 /*bf16*/ * 2 /*K and V*/; }
+    size_t token_bytes() const { return (size_t)items() * head_dim * (held() ? 1 : 2 /*bf16*/) * 2 /*K and V*/; }
+    size_t exps_offset(int layer) const { return layer_offset[layer] + (size_t)layout[layer].capacity * token_bytes(); }
+    HeldRegion held_region(int layer) const
+    {
+        return HeldRegion{reinterpret_cast<uint8_t*>(arena + layer_offset[layer]), reinterpret_cast<int8_t*>(arena + exps_offset(layer)),
+                          layout[layer].capacity};
+    }
     LayerRegion region(int layer) const
     {
         return LayerRegion{reinterpret_cast<__nv_bfloat16*>(arena + layer_offset[layer]), layout[layer].capacity};
@@ -99,8 +107,14 @@ int check_desc(const amskv_desc* d)
         if (d->policy[l].n_condensed < 0 || d->policy[l].n_local < 1) return AMSKV_ERR_INVALID;
         if (d->policy[l].cache_demanding < 0 || d->policy[l].cache_demanding > AMSKV_LAYER_PROMOTABLE) return AMSKV_ERR_INVALID;
     }
-    if ((d->flags & ~(AMSKV_FLAG_PLAN_ONLY | AMSKV_FLAG_BULK_APPEND | AMSKV_FLAG_TRANSIENT_LAST_SCALE | AMSKV_FLAG_NVTX)) != 0)
+    if ((d->flags & ~(AMSKV_FLAG_PLAN_ONLY | AMSKV_FLAG_BULK_APPEND | AMSKV_FLAG_TRANSIENT_LAST_SCALE | AMSKV_FLAG_NVTX |
+                     AMSKV_FLAG_KV_E4M3)) != 0)
         return AMSKV_ERR_INVALID;
+    if (d->flags & AMSKV_FLAG_KV_E4M3) {
+        if (d->flags & (AMSKV_FLAG_BULK_APPEND | AMSKV_FLAG_TRANSIENT_LAST_SCALE)) return AMSKV_ERR_UNSUPPORTED;
+        for (int l = 0; d->token_budget && l < d->layers; ++l)
+            if (d->token_budget[l].budget_tokens != 0) return AMSKV_ERR_UNSUPPORTED;   // budgets cut scales inside their blocks
+    }
     if (!(d->softmax_scale == d->softmax_scale)) return AMSKV_ERR_INVALID;  // NaN
     return AMSKV_OK;
 }
@@ -127,6 +141,10 @@ int plan(const amskv_desc* d, amskv_cache* c)
     c->promoted.assign(d->layers, 0);
     c->layer_offset.resize(d->layers);
     size_t at = kStatusBytes;
+    // held in 8 bits, every scale starts on a block of its own: segments are laid out as if they were whole blocks
+    std::vector<int32_t> room(c->tokens);
+    if (c->held())
+        for (int32_t& t : room) t = (t + kBlock - 1) / kBlock * kBlock;
     for (int l = 0; l < d->layers; ++l) {
         const bool transient_last = (d->flags & AMSKV_FLAG_TRANSIENT_LAST_SCALE) != 0;
         if (d->token_budget && d->token_budget[l].budget_tokens > 0) {
@@ -135,13 +153,14 @@ int plan(const amskv_desc* d, amskv_cache* c)
             c->promotable[l] = c->layout[l].c_promoted > 0;
         } else {
             const bool may_promote = d->policy[l].cache_demanding == AMSKV_LAYER_PROMOTABLE;
-            c->layout[l].build(c->tokens, d->policy[l].n_condensed, d->policy[l].n_local,
+            c->layout[l].build(room, d->policy[l].n_condensed, d->policy[l].n_local,
                                d->policy[l].cache_demanding == AMSKV_LAYER_DEMANDING, transient_last, may_promote);
             c->promotable[l] = may_promote && !c->layout[l].full;
         }
         if ((int64_t)c->layout[l].capacity > (1ll << 30)) return AMSKV_ERR_INVALID;
         c->layer_offset[l] = at;
-        at += align_up((size_t)c->layout[l].capacity * c->token_bytes());
+        at += align_up((size_t)c->layout[l].capacity * c->token_bytes() +
+                       (c->held() ? (size_t)c->items() * 2 * (c->layout[l].capacity / kBlock) : 0));
     }
     c->arena_bytes = at;
     c->layout0 = c->layout;
@@ -332,7 +351,9 @@ int amskv_cache_create(const amskv_desc* desc, void* dev_mem, size_t dev_bytes, 
         return AMSKV_ERR_CUDA;
     }
     c->tc_ready = false;
-    if (tc_supported(c->head_dim) && major == 10) {
+    if (c->held()) {   // (its kernels need no maps of the cache)
+        c->tc_ready = tc_supported(c->head_dim) && major == 10;
+    } else if (tc_supported(c->head_dim) && major == 10) {
         c->k_maps.resize(c->layers);
         c->v_maps.resize(c->layers);
         c->k_maps64.resize(c->layers);
@@ -385,6 +406,13 @@ int amskv_append(amskv_cache* cache, int layer, int scale, const void* K, const 
         if (rc != AMSKV_OK) return rc;
         rc = make_strided(V, strides, cache->rows, cache->heads, T, cache->head_dim, &vs);
         if (rc != AMSKV_OK) return rc;
+        if (cache->held()) {
+            const cudaError_t e = launch_append_held(ks, vs, cache->held_region(layer), lay.offset[scale], T, cache->rows, cache->heads,
+                                                     cache->head_dim, cache->sm_count, static_cast<cudaStream_t>(stream));
+            if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
+            note_appended(cache, layer, scale);
+            return AMSKV_OK;
+        }
         Piece piece[LayerLayout::kMaxPieces];
         const int32_t n_pieces = lay.pieces(cache->tokens, scale, piece);
         for (int32_t i = 0; i < n_pieces; ++i) {
@@ -424,6 +452,7 @@ int amskv_promote_layer(amskv_cache* cache, int layer)
 int amskv_set_attend_path(amskv_cache* cache, int path)
 {
     if (!cache || path < AMSKV_PATH_AUTO || path > AMSKV_PATH_SMALL) return AMSKV_ERR_INVALID;
+    if (cache->held() && path == AMSKV_PATH_SIMT) return AMSKV_ERR_UNSUPPORTED;
     if ((path == AMSKV_PATH_TENSOR || path == AMSKV_PATH_TENSOR_PAIR) && !cache->tc_ready) return AMSKV_ERR_UNSUPPORTED;
     cache->path = path;
     return AMSKV_OK;
@@ -446,8 +475,17 @@ int amskv_attend(amskv_cache* cache, int layer, int scale, const void* Q, void* 
     ranges.n = cache->layout[layer].ranges(cache->tokens, scale, ranges.r);
     ranges.total = 0;
     for (int i = 0; i < ranges.n; ++i) ranges.total += ranges.r[i].len;
-    const AttendKernel kernel = choose_kernel(cache, T, ranges.total);
     cudaError_t e;
+    if (cache->held()) {
+        const HeldRegion region = cache->held_region(layer);
+        HeldKeys keys{region.codes, region.exps, region.capacity, 0, ranges};
+        for (int i = 0; i < ranges.n; ++i) keys.blocks += (ranges.r[i].len + kBlock - 1) / kBlock;
+        e = launch_attend_rows(q, o, keys, T, cache->rows, cache->heads, cache->head_dim, cache->softmax_scale, cache->sm_count,
+                               static_cast<cudaStream_t>(stream));
+        if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
+        return AMSKV_OK;
+    }
+    const AttendKernel kernel = choose_kernel(cache, T, ranges.total);
     if (kernel == AttendKernel::Small) {
         e = launch_attend_small(q, o, cache->region(layer), ranges, T, cache->rows, cache->heads, cache->head_dim,
                                 cache->softmax_scale, cache->sm_count, static_cast<cudaStream_t>(stream));
@@ -490,6 +528,10 @@ int amskv_append_attend(amskv_cache* cache, int layer, int scale, const void* K,
     if (rc == AMSKV_OK) rc = make_strided(Q, q_strides, cache->rows, cache->heads, T, cache->head_dim, &q);
     if (rc == AMSKV_OK) rc = make_strided(out, o_strides, cache->rows, cache->heads, T, cache->head_dim, &o, true);
     if (rc != AMSKV_OK) return rc;
+    if (cache->held()) {
+        rc = amskv_append(cache, layer, scale, K, V, kv_strides, stream);
+        return rc != AMSKV_OK ? rc : amskv_attend(cache, layer, scale, Q, out, q_strides, o_strides, stream);
+    }
     if (cache->transient(scale)) {
         // Never stored: the queries attend to the older retained tokens in the cache and to the scale's own
         // K and V straight from the caller's tensors (paired kernel, else the CUDA-core kernel).
@@ -641,7 +683,7 @@ int amskv_attention_density(amskv_cache* cache, int layer, int scale, const void
                             double* out, size_t out_entries, void* stream)
 {
     if (bad_layer_scale(cache, layer, scale) || !out || (reinterpret_cast<uintptr_t>(out) & 7u)) return AMSKV_ERR_INVALID;
-    if (cache->plan_only()) return AMSKV_ERR_UNSUPPORTED;
+    if (cache->plan_only() || cache->held()) return AMSKV_ERR_UNSUPPORTED;
     if (scale != cache->last_appended[layer]) return AMSKV_ERR_ORDER;
     const int32_t T = cache->tokens[scale];
     Strided q;
@@ -673,7 +715,7 @@ int amskv_attend_density(amskv_cache* cache, int layer, int scale, const void* Q
                          const int64_t o_strides[3], double* density, size_t density_entries, void* stream)
 {
     if (bad_layer_scale(cache, layer, scale) || !density || (reinterpret_cast<uintptr_t>(density) & 7u)) return AMSKV_ERR_INVALID;
-    if (cache->plan_only()) return AMSKV_ERR_UNSUPPORTED;
+    if (cache->plan_only() || cache->held()) return AMSKV_ERR_UNSUPPORTED;
     if (scale != cache->last_appended[layer]) return AMSKV_ERR_ORDER;
     const int32_t T = cache->tokens[scale];
     Strided q, o;
@@ -724,6 +766,53 @@ int amskv_attend_density(amskv_cache* cache, int layer, int scale, const void* Q
     rc = amskv_attend(cache, layer, scale, Q, out, q_strides, o_strides, stream);
     if (rc != AMSKV_OK) return rc;
     return amskv_attention_density(cache, layer, scale, Q, q_strides, density, density_entries, stream);
+}
+
+int amskv_read_segment(amskv_cache* cache, int layer, int segment, void* K, void* V, const int64_t strides[3], void* stream)
+{
+    if (bad_layer_scale(cache, layer, segment)) return AMSKV_ERR_INVALID;
+    const CallRange range(cache, "amskv_read_segment", layer, segment);
+    const LayerLayout& lay = cache->layout[layer];
+    if (lay.token_mode) return AMSKV_ERR_UNSUPPORTED;
+    if (cache->last_appended[layer] < 0 || !lay.keeps(segment, cache->last_appended[layer])) return AMSKV_ERR_ORDER;
+    const int32_t T = cache->tokens[segment];
+    Strided k, v;
+    int rc = make_strided(K, strides, cache->rows, cache->heads, T, cache->head_dim, &k, true);
+    if (rc == AMSKV_OK) rc = make_strided(V, strides, cache->rows, cache->heads, T, cache->head_dim, &v, true);
+    if (rc != AMSKV_OK) return rc;
+    if (cache->plan_only()) return AMSKV_ERR_UNSUPPORTED;
+    const int8_t* exps = cache->held() ? cache->held_region(layer).exps : nullptr;
+    const cudaError_t e = launch_read_segment(cache->arena + cache->layer_offset[layer], exps, lay.capacity, lay.offset[segment], T,
+                                              cache->rows, cache->heads, cache->head_dim, k, v, cache->sm_count,
+                                              static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
+    return AMSKV_OK;
+}
+
+int amskv_cross_attend(amskv_cache* cache, int scale, const amskv_encoder* enc, const void* K, const void* V, const int64_t kv_strides[3],
+                       const void* Q, void* out, const int64_t q_strides[3], const int64_t o_strides[3], void* stream)
+{
+    if (bad_layer_scale(cache, 0, scale) || !enc) return AMSKV_ERR_INVALID;
+    const CallRange range(cache, "amskv_cross_attend", 0, scale);
+    if (enc->kv_heads < 1 || cache->heads % enc->kv_heads || enc->keys < 1 || enc->max_keys < 0 || (enc->lengths && enc->offsets)) return AMSKV_ERR_INVALID;
+    if ((reinterpret_cast<uintptr_t>(enc->lengths) & 3u) || (reinterpret_cast<uintptr_t>(enc->offsets) & 3u)) return AMSKV_ERR_INVALID;
+    if (enc->keys > (1 << 30)) return AMSKV_ERR_UNSUPPORTED;
+    const int32_t T = cache->tokens[scale];
+    Strided k, v, q, o;
+    // (packed keys have no row dimension; the same keys for all rows, a row stride of 0, are read as they are)
+    const int32_t kv_rows = enc->offsets || (kv_strides && kv_strides[0] == 0) ? 1 : cache->rows;
+    int rc = make_strided(K, kv_strides, kv_rows, enc->kv_heads, enc->keys, cache->head_dim, &k);
+    if (rc == AMSKV_OK) rc = make_strided(V, kv_strides, kv_rows, enc->kv_heads, enc->keys, cache->head_dim, &v);
+    if (rc == AMSKV_OK) rc = make_strided(Q, q_strides, cache->rows, cache->heads, T, cache->head_dim, &q);
+    if (rc == AMSKV_OK) rc = make_strided(out, o_strides, cache->rows, cache->heads, T, cache->head_dim, &o, true);
+    if (rc != AMSKV_OK) return rc;
+    if (cache->plan_only()) return AMSKV_ERR_UNSUPPORTED;
+    const EncoderKeys keys{static_cast<const __nv_bfloat16*>(k.ptr), static_cast<const __nv_bfloat16*>(v.ptr), k.row, k.head, k.token,
+                           enc->lengths, enc->offsets, enc->keys, enc->max_keys > 0 ? std::min(enc->max_keys, enc->keys) : enc->keys};
+    const cudaError_t e = launch_attend_rows(q, o, keys, T, cache->rows, enc->kv_heads, cache->heads / enc->kv_heads, cache->head_dim,
+                                             cache->softmax_scale, cache->sm_count, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
+    return AMSKV_OK;
 }
 
 int amskv_step_staging_bytes(const amskv_cache* cache, size_t* bytes)

@@ -1,0 +1,189 @@
+"""Cross attention to an encoder's states on the GPU against the definition in 64 bits.
+
+Tolerance, element by element: half a step of bf16 of the output (2^-8), and the probabilities' rounding to bf16, 2^-8 of the sum
+of p |v|, and the exponentials' own error, 2^-10 at most (a cubic in one kernel; the special-function unit's is 2^-22), of the same
+sum in numerator and denominator."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_common import Cache
+from oracle import operators as ref
+from paper_2511_16047_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+PATHS = {"auto": B.PATH_AUTO, "rows": B.PATH_SMALL, "tiles": B.PATH_TENSOR_PAIR}
+
+
+def _np(x):
+    return x.detach().cpu().double().numpy()
+
+
+def _check(out, q, keys, group, scale, what):
+    """keys[r] = (k, v) of row r: [kv_heads, n, D] in 64 bits."""
+    got = _np(out)
+    for r, (k, v) in enumerate(keys):
+        k, v = np.repeat(k, group, 0), np.repeat(v, group, 0)
+        want, size = ref.attention(_np(q[r]), k, v, scale)
+        tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -9) * size
+        assert (np.abs(got[r] - want) <= tol).all(), (what, r, np.abs(got[r] - want).max(), (np.abs(got[r] - want) / (tol + 1e-30)).max())
+
+
+def _lengths(rows, keys):
+    """None, one, a few, one short of a block, of a tile, all."""
+    pool = [keys, 0, 1, min(15, keys), min(17, keys), min(63, keys), min(65, keys), (keys + 1) // 2, max(keys - 1, 0)]
+    return [pool[r % len(pool)] for r in range(rows)]
+
+
+SHAPES = [
+    # rows, heads, kv_heads, D, side, keys
+    (1, 1, 1, 64, 1, 1),
+    (2, 16, 16, 128, 1, 77),
+    (9, 4, 2, 64, 1, 200),
+    (9, 8, 2, 128, 2, 130),        # a group of heads fills one block of query rows
+    (3, 6, 2, 64, 3, 64),          # 27 rows of a group: two blocks
+    (9, 3, 3, 64, 5, 77),
+    (9, 4, 4, 128, 6, 512),
+    (2, 5, 1, 64, 7, 40),
+    (4, 3, 3, 64, 11, 129),        # 121 queries: one tile
+    (4, 3, 3, 128, 11, 300),
+    (5, 5, 5, 64, 13, 81),         # 169 queries: two tiles, an odd number of heads
+    (5, 3, 1, 128, 13, 190),
+    (9, 3, 3, 64, 18, 333),        # 324 queries: three tiles
+    (3, 3, 3, 128, 20, 65),
+    (2, 2, 2, 128, 32, 1100),
+]
+
+
+@pytest.mark.parametrize("path", sorted(PATHS))
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_rows_of_different_lengths(shape, path):
+    rows, heads, kv, D, side, keys = shape
+    T, group = side * side, heads // kv
+    g = torch.Generator(device="cuda").manual_seed(sum(shape))
+    q = torch.randn(rows, heads, T, D, generator=g, device="cuda").bfloat16()
+    lengths = _lengths(rows, keys)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    k, v = (torch.randn(rows, kv, keys, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    behind = torch.arange(keys, device="cuda")[None] >= n[:, None]
+    k[behind[:, None].expand(rows, kv, keys)] = float("nan")       # what lies behind a row's last key is never looked at
+    v[behind[:, None].expand(rows, kv, keys)] = float("inf")
+    want = [(_np(k[r, :, :m]), _np(v[r, :, :m])) for r, m in enumerate(lengths)]
+    scale = 1.0 / math.sqrt(D)
+    with Cache(1, heads, D, rows, (side,), [(0, 1, False)]) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+        out = torch.full_like(q, float("nan"))
+        B.amskv_cross_attend(c.h, 0, kv, keys, k, v, q, out, lengths=n)
+        assert B.amskv_status(c.h) == 0
+        _check(out, q, want, group, scale, "padded")
+        again = torch.full_like(q, float("nan"))
+        B.amskv_cross_attend(c.h, 0, kv, keys, k, v, q, again, lengths=n)
+        assert torch.equal(out, again)
+
+        # packed, all tensors views of what projections leave, and guard values around the output
+        total = sum(lengths)
+        kv2 = torch.full((total + 3, 2, kv, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        at = 0
+        for r, m in enumerate(lengths):
+            kv2[at:at + m, 0], kv2[at:at + m, 1] = k[r, :, :m].transpose(0, 1), v[r, :, :m].transpose(0, 1)
+            at += m
+        off = torch.tensor(np.concatenate([[0], np.cumsum(lengths)]), dtype=torch.int32, device="cuda")
+        kp, vp = (kv2[:, i].transpose(0, 1)[None] for i in range(2))
+        qv = q.transpose(1, 2).contiguous().transpose(1, 2)
+        big = torch.full((rows, T + 1, heads + 1, D), 7.0, dtype=torch.bfloat16, device="cuda")
+        ov = big[:, :T, 1:].transpose(1, 2)
+        B.amskv_cross_attend(c.h, 0, kv, total + 3, kp, vp, qv, ov, offsets=off, max_keys=max(lengths))
+        assert B.amskv_status(c.h) == 0
+        _check(ov, q, want, group, scale, "packed")
+        assert (big[:, T] == 7.0).all() and (big[:, :, 0] == 7.0).all()
+
+
+@pytest.mark.parametrize("path", sorted(PATHS))
+def test_all_keys_the_same_keys_for_all_rows_and_cut_lengths(path):
+    rows, heads, kv, D, side, keys = 3, 4, 2, 64, 12, 100
+    q = torch.randn(rows, heads, side * side, D, device="cuda").bfloat16()
+    k, v = (torch.randn(1, kv, keys, D, device="cuda").bfloat16() for _ in range(2))
+    with Cache(1, heads, D, rows, (side,), [(0, 1, False)], softmax_scale=0.3) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+
+        def run(**kw):
+            out = torch.full_like(q, float("nan"))
+            B.amskv_cross_attend(c.h, 0, kv, keys, kk, vv, q, out, **kw)
+            assert B.amskv_status(c.h) == 0
+            return out
+
+        def want(counts, firsts=(0, 0, 0)):
+            return [(_np(kk[r % kk.shape[0], :, f:f + n]), _np(vv[r % kk.shape[0], :, f:f + n])) for r, (n, f) in enumerate(zip(counts, firsts))]
+
+        kk, vv = k.expand(rows, kv, keys, D), v.expand(rows, kv, keys, D)
+        _check(run(), q, want([100] * 3), 2, 0.3, "broadcast")
+        kk, vv = kk.contiguous(), vv.contiguous()
+        _check(run(), q, want([100] * 3), 2, 0.3, "all keys")
+        _check(run(max_keys=70), q, want([70] * 3), 2, 0.3, "cut to max_keys")
+        odd = torch.tensor([-5, 1 << 30, 33], dtype=torch.int32, device="cuda")     # lengths outside the tensor are cut to it
+        _check(run(lengths=odd), q, want([0, 100, 33]), 2, 0.3, "odd lengths")
+        kk, vv = k, v
+        off = torch.tensor([-7, 20, 12, 1 << 30], dtype=torch.int32, device="cuda")  # from 0 to 20, none, from 12 to the end
+        _check(run(offsets=off), q, want([20, 0, 88], [0, 0, 12]), 2, 0.3, "odd offsets")
+        off = torch.tensor([2 ** 31 - 1, -2 ** 31, 100, 100], dtype=torch.int32, device="cuda")
+        _check(run(offsets=off), q, want([0, 100, 0], [0, 0, 0]), 2, 0.3, "offsets in no order")
+
+
+@pytest.mark.parametrize("path", sorted(PATHS))
+@pytest.mark.parametrize("D", [64, 128])
+def test_peaked_logits_and_large_values(path, D):
+    """Logits tens apart, growing from tile to tile so that the reference has to move, and values of very different sizes."""
+    rows, heads, side, keys = 2, 2, 14, 400
+    g = torch.Generator(device="cuda").manual_seed(D)
+    q = (6.0 * torch.randn(rows, heads, side * side, D, generator=g, device="cuda")).bfloat16()
+    k = torch.randn(rows, heads, keys, D, generator=g, device="cuda")
+    k = (k * (torch.arange(keys, device="cuda")[:, None] / 100.0)).bfloat16()
+    v = (torch.randn(rows, heads, keys, D, generator=g, device="cuda") * torch.exp2(torch.randint(-20, 20, (1, 1, keys, 1), generator=g, device="cuda").float())).bfloat16()
+    with Cache(1, heads, D, rows, (side,), [(0, 1, False)]) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+        out = torch.full_like(q, float("nan"))
+        B.amskv_cross_attend(c.h, 0, heads, keys, k, v, q, out)
+        assert B.amskv_status(c.h) == 0
+        _check(out, q, [(_np(k[r]), _np(v[r])) for r in range(rows)], 1, 1.0 / math.sqrt(D), "peaked")
+
+
+def test_the_cache_is_left_alone_and_order_does_not_matter():
+    """Cross attention between the steps of a layer, on another stream, and captured: the cache's own results stay the same."""
+    sides, heads, D, rows, keys = (1, 2, 4), 2, 64, 2, 33
+    steps = [[torch.randn(rows, heads, s * s, D, device="cuda").bfloat16() for _ in range(3)] for s in sides]
+    k, v = (torch.randn(rows, heads, keys, D, device="cuda").bfloat16() for _ in range(2))
+    with Cache(1, heads, D, rows, sides, [(0, 1, True)]) as c:
+        outs = []
+        for cross in (False, True):
+            B.amskv_cache_reset(c.h)
+            outs.append([])
+            for i, (q, kk, vv) in enumerate(steps):
+                o = torch.empty_like(q)
+                B.amskv_append_attend(c.h, 0, i, kk, vv, q, o)
+                outs[-1].append(o)
+                if cross:
+                    for s in range(len(sides)):
+                        x = torch.full_like(steps[s][0], float("nan"))
+                        B.amskv_cross_attend(c.h, s, heads, keys, k, v, steps[s][0], x)
+                        _check(x, steps[s][0], [(_np(k[r]), _np(v[r])) for r in range(rows)], 1, 0.125, "between steps")
+        for a, b in zip(*outs):
+            assert torch.equal(a, b)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        q = steps[2][0]
+        x = torch.empty_like(q)
+        B.amskv_cross_attend(c.h, 2, heads, keys, k, v, q, x, stream=side)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            B.amskv_cross_attend(c.h, 2, heads, keys, k, v, q, x, stream=side)
+        q.copy_(torch.randn_like(q))
+        k.copy_(torch.randn_like(k))
+        x.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(x, q, [(_np(k[r]), _np(v[r])) for r in range(rows)], 1, 0.125, "replayed")
+        assert B.amskv_status(c.h) == 0
