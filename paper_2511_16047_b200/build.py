@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libamskv.so")
 STEPS = os.path.join(HERE, "_steps" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 STEPS_SOURCE = os.path.join(CSRC, "steps.c")
-SOURCES = ["api.cu", "append.cu", "attend_simt.cu", "attend_tc.cu", "attend_pair.cu", "attend_small.cu", "attend_mid.cu", "similarity.cu", "density.cu", "rotary.cu", "held.cu", "attend_rows.cu", "selftest.cu"]
+SOURCES = ["api.cu", "append.cu", "attend_simt.cu", "attend_tc.cu", "attend_pair.cu", "attend_small.cu", "attend_mid.cu", "similarity.cu", "density.cu", "rotary.cu", "held.cu", "attend_rows.cu", "attend_tiles.cu", "selftest.cu"]
 HEADERS = ["kernels.cuh", "keys.cuh", "policy.hpp", "sm100_ptx.cuh", os.path.join("..", "..", "include", "amskv.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr"]

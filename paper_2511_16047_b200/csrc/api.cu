@@ -267,6 +267,15 @@ void note_appended(amskv_cache* cache, int layer, int scale)
     cache->last_appended[layer] = scale;
 }
 
+// whether the tensor-memory kernel serves a call over an encoder's states or a cache held in 8 bits, else the warp-matrix kernel
+bool takes_tiles(const amskv_cache* cache, int32_t T, int32_t group, int32_t kv_heads, int64_t keys)
+{
+    (void)group, (void)kv_heads, (void)keys;
+    if (!cache->tc_ready || cache->path == AMSKV_PATH_SMALL || cache->path == AMSKV_PATH_SIMT) return false;
+    if (cache->path != AMSKV_PATH_AUTO) return true;
+    return T > 64;
+}
+
 // which kernel amskv_attend uses for T query tokens over `total` keys
 enum class AttendKernel { Small, Mid, Simt, Pair, Tensor };
 // (copies: the call includes an append that is not one contiguous copy; see mid_preferred)
@@ -480,8 +489,12 @@ int amskv_attend(amskv_cache* cache, int layer, int scale, const void* Q, void* 
         const HeldRegion region = cache->held_region(layer);
         HeldKeys keys{region.codes, region.exps, region.capacity, 0, ranges};
         for (int i = 0; i < ranges.n; ++i) keys.blocks += (ranges.r[i].len + kBlock - 1) / kBlock;
-        e = launch_attend_rows(q, o, keys, T, cache->rows, cache->heads, cache->head_dim, cache->softmax_scale, cache->sm_count,
-                               static_cast<cudaStream_t>(stream));
+        if (takes_tiles(cache, T, 1, cache->heads, (int64_t)keys.blocks * kBlock))
+            e = launch_attend_tiles(q, o, keys, T, cache->rows, cache->heads, cache->head_dim, cache->softmax_scale, cache->status_word(),
+                                    cache->sm_count, static_cast<cudaStream_t>(stream));
+        else
+            e = launch_attend_rows(q, o, keys, T, cache->rows, cache->heads, cache->head_dim, cache->softmax_scale, cache->sm_count,
+                                   static_cast<cudaStream_t>(stream));
         if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
         return AMSKV_OK;
     }
@@ -809,8 +822,12 @@ int amskv_cross_attend(amskv_cache* cache, int scale, const amskv_encoder* enc, 
     if (cache->plan_only()) return AMSKV_ERR_UNSUPPORTED;
     const EncoderKeys keys{static_cast<const __nv_bfloat16*>(k.ptr), static_cast<const __nv_bfloat16*>(v.ptr), k.row, k.head, k.token,
                            enc->lengths, enc->offsets, enc->keys, enc->max_keys > 0 ? std::min(enc->max_keys, enc->keys) : enc->keys};
-    const cudaError_t e = launch_attend_rows(q, o, keys, T, cache->rows, enc->kv_heads, cache->heads / enc->kv_heads, cache->head_dim,
-                                             cache->softmax_scale, cache->sm_count, static_cast<cudaStream_t>(stream));
+    const int32_t group = cache->heads / enc->kv_heads;
+    const cudaError_t e = takes_tiles(cache, T, group, enc->kv_heads, keys.max_keys)
+        ? launch_attend_tiles(q, o, keys, T, cache->rows, enc->kv_heads, group, cache->head_dim, cache->softmax_scale, cache->status_word(),
+                              cache->sm_count, static_cast<cudaStream_t>(stream))
+        : launch_attend_rows(q, o, keys, T, cache->rows, enc->kv_heads, group, cache->head_dim, cache->softmax_scale, cache->sm_count,
+                             static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
     return AMSKV_OK;
 }

@@ -206,6 +206,12 @@ cudaError_t launch_attend_rows(const Strided& Q, const Strided& O, const Encoder
 cudaError_t launch_attend_rows(const Strided& Q, const Strided& O, const HeldKeys& held, int32_t T, int32_t rows, int32_t heads,
                                int32_t D, float softmax_scale, int sm_count, cudaStream_t stream);
 
+// Tensor-memory kernel over either (attend_tiles.cu).
+cudaError_t launch_attend_tiles(const Strided& Q, const Strided& O, const EncoderKeys& enc, int32_t T, int32_t rows, int32_t kv_heads,
+                                int32_t group, int32_t D, float softmax_scale, int* status, int sm_count, cudaStream_t stream);
+cudaError_t launch_attend_tiles(const Strided& Q, const Strided& O, const HeldKeys& held, int32_t T, int32_t rows, int32_t heads,
+                                int32_t D, float softmax_scale, int* status, int sm_count, cudaStream_t stream);
+
 // One warp whose bounded wait runs out after `limit` iterations (nothing ever arrives): records
 // kStatusSyncTimeout in *status and returns normally.
 cudaError_t launch_wait_gives_up(uint32_t limit, int* status, cudaStream_t stream);
