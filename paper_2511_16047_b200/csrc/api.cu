@@ -58,10 +58,10 @@ struct amskv_cache {
     bool transient(int scale) const { return (flags & AMSKV_FLAG_TRANSIENT_LAST_SCALE) != 0 && scale == n_scales - 1; }
     int64_t items() const { return (int64_t)rows * heads; }
     size_t token_bytes() const { return (size_t)items() * head_dim * (held() ? 1 : 2 /*bf16*/) * 2 /*K and V*/; }
-    size_t exps_offset(int layer) const { return layer_offset[layer] + (size_t)layout[layer].capacity * token_bytes(); }
+    size_t scales_offset(int layer) const { return layer_offset[layer] + (size_t)layout[layer].capacity * token_bytes(); }
     HeldRegion held_region(int layer) const
     {
-        return HeldRegion{reinterpret_cast<uint8_t*>(arena + layer_offset[layer]), reinterpret_cast<int8_t*>(arena + exps_offset(layer)),
+        return HeldRegion{reinterpret_cast<uint8_t*>(arena + layer_offset[layer]), reinterpret_cast<uint32_t*>(arena + scales_offset(layer)),
                           layout[layer].capacity};
     }
     LayerRegion region(int layer) const
@@ -160,7 +160,7 @@ int plan(const amskv_desc* d, amskv_cache* c)
         if ((int64_t)c->layout[l].capacity > (1ll << 30)) return AMSKV_ERR_INVALID;
         c->layer_offset[l] = at;
         at += align_up((size_t)c->layout[l].capacity * c->token_bytes() +
-                       (c->held() ? (size_t)c->items() * 2 * (c->layout[l].capacity / kBlock) : 0));
+                       (c->held() ? (size_t)c->items() * (c->layout[l].capacity / kBlock) * sizeof(uint32_t) : 0));
     }
     c->arena_bytes = at;
     c->layout0 = c->layout;
@@ -487,7 +487,7 @@ int amskv_attend(amskv_cache* cache, int layer, int scale, const void* Q, void* 
     cudaError_t e;
     if (cache->held()) {
         const HeldRegion region = cache->held_region(layer);
-        HeldKeys keys{region.codes, region.exps, region.capacity, 0, ranges};
+        HeldKeys keys{region.codes, region.scales, region.capacity, 0, ranges};
         for (int i = 0; i < ranges.n; ++i) keys.blocks += (ranges.r[i].len + kBlock - 1) / kBlock;
         if (takes_tiles(cache, T, 1, cache->heads, (int64_t)keys.blocks * kBlock))
             e = launch_attend_tiles(q, o, keys, T, cache->rows, cache->heads, cache->head_dim, cache->softmax_scale, cache->status_word(),
@@ -794,8 +794,8 @@ int amskv_read_segment(amskv_cache* cache, int layer, int segment, void* K, void
     if (rc == AMSKV_OK) rc = make_strided(V, strides, cache->rows, cache->heads, T, cache->head_dim, &v, true);
     if (rc != AMSKV_OK) return rc;
     if (cache->plan_only()) return AMSKV_ERR_UNSUPPORTED;
-    const int8_t* exps = cache->held() ? cache->held_region(layer).exps : nullptr;
-    const cudaError_t e = launch_read_segment(cache->arena + cache->layer_offset[layer], exps, lay.capacity, lay.offset[segment], T,
+    const uint32_t* scales = cache->held() ? cache->held_region(layer).scales : nullptr;
+    const cudaError_t e = launch_read_segment(cache->arena + cache->layer_offset[layer], scales, lay.capacity, lay.offset[segment], T,
                                               cache->rows, cache->heads, cache->head_dim, k, v, cache->sm_count,
                                               static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }

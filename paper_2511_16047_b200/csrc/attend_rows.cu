@@ -67,12 +67,12 @@ __device__ __forceinline__ float2 ld_cluster_8B(uint32_t addr)
     return v;
 }
 
-// Codes of one chunk on their way: a thread's 16-byte pieces of K and V, and the powers of two of their blocks.
+// Codes of one chunk on their way: a thread's 16-byte pieces of K and V, and the scale words of their blocks.
 template <int D>
 struct HeldPieces {
     static constexpr int kPieces = D / 16, kRows = kThreads / kPieces, kN = kChunk / kRows;   // pieces of a row, rows of a pass, passes
     uint4 k[kN], v[kN];
-    int32_t ke[kN], ve[kN];
+    uint32_t scale[kN];
 };
 
 template <int D, int kQB, bool kHeld>
@@ -106,7 +106,7 @@ attend_rows_kernel(const __nv_bfloat16* Q, int64_t q_row, int64_t q_head, int64_
     const uint4* q0 = reinterpret_cast<const uint4*>(qbase + row_offset(min(m0 + g, M - 1), q_head, q_tok) + 8 * q);
     const uint4* q1 = reinterpret_cast<const uint4*>(qbase + row_offset(min(m0 + g + 8, M - 1), q_head, q_tok) + 8 * q);
     overlap_with_previous();
-    EncoderView ev(enc, row, kv_head);
+    EncoderView ev(enc, row, kv_head, EncoderBounds(enc, row));
     HeldView hv(held, item, D);
     const int32_t blocks = kHeld ? hv.blocks() : ev.blocks();
     // this CTA's chunks
@@ -147,14 +147,13 @@ attend_rows_kernel(const __nv_bfloat16* Q, int64_t q_row, int64_t q_head, int64_
             const int r = w_row + i * Pieces::kRows;
             const int32_t b = c * (kChunk / kBlock) + r / kBlock, slot = r % kBlock;
             next.k[i] = next.v[i] = make_uint4(0, 0, 0, 0);
-            next.ke[i] = next.ve[i] = 0;
+            next.scale[i] = 0;
             if (slot < fetch.valid(b)) {
                 const int32_t pos = fetch.position(b);
                 const uint8_t* src = fetch.codes + (int64_t)(pos + slot) * D + w_piece * 16;
                 next.k[i] = load_16B(src);
                 next.v[i] = load_16B(src + (int64_t)fetch.capacity * D);
-                next.ke[i] = load_exponent(fetch.exps + pos / kBlock);
-                next.ve[i] = load_exponent(fetch.exps + (fetch.capacity + pos) / kBlock);
+                next.scale[i] = load_word(fetch.scales + pos / kBlock);
             }
         }
     };
@@ -164,11 +163,11 @@ attend_rows_kernel(const __nv_bfloat16* Q, int64_t q_row, int64_t q_head, int64_
         for (int i = 0; i < Pieces::kN; ++i) {
             const int r = w_row + i * Pieces::kRows;
             uint4 lo, hi;
-            widen16(next.k[i], power_of_two(next.ke[i]), lo, hi);
+            widen16(next.k[i], next.scale[i], false, lo, hi);
             uint8_t* kt = st + r * C::kRowBytes;
             *reinterpret_cast<uint4*>(kt + (((2 * w_piece) ^ ((r & 1) << 2)) << 4)) = lo;
             *reinterpret_cast<uint4*>(kt + (((2 * w_piece + 1) ^ ((r & 1) << 2)) << 4)) = hi;
-            widen16(next.v[i], power_of_two(next.ve[i]), lo, hi);
+            widen16(next.v[i], next.scale[i], true, lo, hi);
             uint8_t* vt = st + C::kTileBytes + r * C::kRowBytes;
             *reinterpret_cast<uint4*>(vt + (((2 * w_piece) ^ (r & 7)) << 4)) = lo;
             *reinterpret_cast<uint4*>(vt + (((2 * w_piece + 1) ^ (r & 7)) << 4)) = hi;

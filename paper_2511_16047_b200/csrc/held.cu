@@ -35,7 +35,7 @@ __device__ __forceinline__ uint2 codes_of(const uint4& x, float inv)
 template <int D>
 __global__ void __launch_bounds__(kThreads)
 append_held_kernel(const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t k_row, int64_t k_head, int64_t k_tok, int64_t v_row,
-                   int64_t v_head, int64_t v_tok, uint8_t* codes, int8_t* exps, int32_t capacity, int32_t offset, int32_t T,
+                   int64_t v_head, int64_t v_tok, uint8_t* codes, uint32_t* scales, int32_t capacity, int32_t offset, int32_t T,
                    int32_t heads, int64_t items)
 {
     constexpr int kPieces = D / 8, kN = kBlock * kPieces / 32;   // 16-byte pieces of a token; of a lane
@@ -56,6 +56,7 @@ append_held_kernel(const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t k_row
                 x[kv][i] = tok < T ? load_16B_once(src + tok * (kv ? v_tok : k_tok) + p % kPieces * 8) : make_uint4(0, 0, 0, 0);
             }
         }
+        int32_t power[2];
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
             uint32_t top = 0;
@@ -71,15 +72,16 @@ append_held_kernel(const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t k_row
                 const int p = i * 32 + lane;
                 if (b * kBlock + p / kPieces < T) *reinterpret_cast<uint2*>(dst + p * 8) = codes_of(x[kv][i], inv);
             }
-            if (lane == 0) exps[(item * 2 + kv) * (int64_t)(capacity / kBlock) + offset / kBlock + b] = (int8_t)e;
+            power[kv] = e;
         }
+        if (lane == 0) scales[item * (capacity / kBlock) + offset / kBlock + b] = scale_word(power[0], power[1]);
     }
 }
 
 // 16 codes, or 8 bf16 values, a thread: K, then V.
 template <bool kHeld>
 __global__ void __launch_bounds__(kThreads)
-read_segment_kernel(const void* region, const int8_t* exps, int32_t capacity, int32_t offset, int32_t T, int32_t D, int32_t heads,
+read_segment_kernel(const void* region, const uint32_t* scales, int32_t capacity, int32_t offset, int32_t T, int32_t D, int32_t heads,
                     int64_t items, __nv_bfloat16* K, __nv_bfloat16* V, int64_t row_stride, int64_t head_stride, int64_t tok_stride)
 {
     constexpr int kValues = kHeld ? 16 : 8;
@@ -95,7 +97,7 @@ read_segment_kernel(const void* region, const int8_t* exps, int32_t capacity, in
         uint4* dst = reinterpret_cast<uint4*>((kv ? V : K) + row * row_stride + head * head_stride + tok * tok_stride + piece * kValues);
         if (kHeld) {
             uint4 lo, hi;
-            widen16(x, power_of_two(load_exponent(exps + half * (capacity / kBlock) + (offset + tok) / kBlock)), lo, hi);
+            widen16(x, load_word(scales + item * (capacity / kBlock) + (offset + tok) / kBlock), kv != 0, lo, hi);
             dst[0] = lo;
             dst[1] = hi;
         } else {
@@ -113,17 +115,17 @@ cudaError_t launch_append_held(const Strided& K, const Strided& V, const HeldReg
     const int64_t blocks = std::min<int64_t>((total + kWarps - 1) / kWarps, 64ll * sm_count);
     auto* kernel = D == 64 ? append_held_kernel<64> : append_held_kernel<128>;
     return launch_kernel(true, kernel, dim3((unsigned)blocks), dim3(kThreads), KernelMemory(0), stream, (const __nv_bfloat16*)K.ptr,
-                         (const __nv_bfloat16*)V.ptr, K.row, K.head, K.token, V.row, V.head, V.token, region.codes, region.exps,
+                         (const __nv_bfloat16*)V.ptr, K.row, K.head, K.token, V.row, V.head, V.token, region.codes, region.scales,
                          region.capacity, offset, T, heads, items);
 }
 
-cudaError_t launch_read_segment(const void* region, const int8_t* exps, int32_t capacity, int32_t offset, int32_t T, int32_t rows,
+cudaError_t launch_read_segment(const void* region, const uint32_t* scales, int32_t capacity, int32_t offset, int32_t T, int32_t rows,
                                 int32_t heads, int32_t D, const Strided& K, const Strided& V, int sm_count, cudaStream_t stream)
 {
-    const int64_t items = (int64_t)rows * heads, total = items * 2 * T * (D / (exps ? 16 : 8));
+    const int64_t items = (int64_t)rows * heads, total = items * 2 * T * (D / (scales ? 16 : 8));
     const int64_t blocks = std::min<int64_t>((total + kThreads - 1) / kThreads, 64ll * sm_count);
-    auto* kernel = exps ? read_segment_kernel<true> : read_segment_kernel<false>;
-    return launch_kernel(true, kernel, dim3((unsigned)blocks), dim3(kThreads), KernelMemory(0), stream, region, exps, capacity, offset, T, D,
+    auto* kernel = scales ? read_segment_kernel<true> : read_segment_kernel<false>;
+    return launch_kernel(true, kernel, dim3((unsigned)blocks), dim3(kThreads), KernelMemory(0), stream, region, scales, capacity, offset, T, D,
                          heads, items, (__nv_bfloat16*)K.ptr, (__nv_bfloat16*)V.ptr, K.row, K.head, K.token);
 }
 

@@ -183,22 +183,23 @@ struct EncoderKeys {
     const int32_t *lengths, *offsets;
     int32_t keys, max_keys;      // extent of the tensor; the most that a row has
 };
-// A layer's region held in 8 bits: item i owns 2 * capacity * D codes, keys first, and 2 * capacity / 16 powers of two.
+// A layer's region held in 8 bits: item i owns 2 * capacity * D codes, keys first, and capacity / 16 words with the powers of two of
+// a block's keys and values.
 struct HeldRegion {
     uint8_t* codes;
-    int8_t* exps;
+    uint32_t* scales;
     int32_t capacity;            // tokens per item, a multiple of 16
 };
 struct HeldKeys {
     const uint8_t* codes;
-    const int8_t* exps;
+    const uint32_t* scales;
     int32_t capacity, blocks;    // blocks of 16 slots that the ranges cover
     RangeList ranges;            // each starts on a block
 };
 cudaError_t launch_append_held(const Strided& K, const Strided& V, const HeldRegion& region, int32_t offset, int32_t T, int32_t rows,
                                int32_t heads, int32_t D, int sm_count, cudaStream_t stream);
-// Positions offset .. offset + T - 1 of a layer's region (of bf16 values: exps null) to [rows, heads, T, D] tensors; K's strides hold for V.
-cudaError_t launch_read_segment(const void* region, const int8_t* exps, int32_t capacity, int32_t offset, int32_t T, int32_t rows,
+// Positions offset .. offset + T - 1 of a layer's region (of bf16 values: scales null) to [rows, heads, T, D] tensors; K's strides hold for V.
+cudaError_t launch_read_segment(const void* region, const uint32_t* scales, int32_t capacity, int32_t offset, int32_t T, int32_t rows,
                                 int32_t heads, int32_t D, const Strided& K, const Strided& V, int sm_count, cudaStream_t stream);
 // Warp-matrix kernel over either (attend_rows.cu); `group` query heads share a key/value head.
 cudaError_t launch_attend_rows(const Strided& Q, const Strided& O, const EncoderKeys& enc, int32_t T, int32_t rows, int32_t kv_heads,
@@ -308,6 +309,12 @@ __device__ __forceinline__ float4 load_float4(const void* p)
 {
     float4 v;
     asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t load_word(const uint32_t* p)
+{
+    uint32_t v;
+    asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p));
     return v;
 }
 __device__ __forceinline__ int32_t load_int(const int32_t* p)

@@ -10,24 +10,36 @@ namespace amskv {
 constexpr int kBlock = 16;   // slots of a block
 
 #ifdef __CUDACC__
+// What the device knows of a row's keys, as loaded; made use of later, so that the loads can run ahead of it.
+struct EncoderBounds {
+    int32_t a = 0, b = 0;
+
+    __device__ __forceinline__ EncoderBounds(const EncoderKeys& e, int32_t row)
+    {
+        if (e.offsets) {
+            a = load_int(e.offsets + row);
+            b = load_int(e.offsets + row + 1);
+        } else if (e.lengths) {
+            b = load_int(e.lengths + row);
+        } else {
+            b = e.keys;
+        }
+    }
+    // (whatever is found there, nothing outside the tensor is read)
+    __device__ __forceinline__ int32_t first(const EncoderKeys& e) const { return min(max(a, 0), e.keys); }
+    __device__ __forceinline__ int32_t len(const EncoderKeys& e) const { return min(min(max(b, first(e)), e.keys) - first(e), e.max_keys); }
+};
 // The keys of one (row, key/value head) of an encoder.
 struct EncoderView {
     const __nv_bfloat16 *k, *v;
     int64_t tok;
     int32_t len;
 
-    __device__ __forceinline__ EncoderView(const EncoderKeys& e, int32_t row, int32_t kv_head)
+    __device__ __forceinline__ EncoderView(const EncoderKeys& e, int32_t row, int32_t kv_head, const EncoderBounds& bounds)
     {
-        int32_t first = 0, end = e.keys;
-        if (e.offsets) {   // (whatever is found there, nothing outside the tensor is read)
-            first = min(max(load_int(e.offsets + row), 0), e.keys);
-            end = min(max(load_int(e.offsets + row + 1), first), e.keys);
-        } else if (e.lengths) {
-            end = min(max(load_int(e.lengths + row), 0), e.keys);
-        }
-        len = min(end - first, e.max_keys);
+        len = bounds.len(e);
         tok = e.tok;
-        const int64_t at = (e.offsets ? 0 : row * e.row) + kv_head * e.head + first * e.tok;
+        const int64_t at = (e.offsets ? 0 : row * e.row) + kv_head * e.head + bounds.first(e) * e.tok;
         k = e.K + at;
         v = e.V + at;
     }
@@ -39,14 +51,21 @@ struct EncoderView {
 struct HeldView {
     const RangeList& ranges;
     const uint8_t* codes;      // [capacity][D] keys, values behind them
-    const int8_t* exps;        // [capacity / 16] of the keys, of the values behind them
+    const uint32_t* scales;    // [capacity / 16]
     int32_t capacity, total;
     int32_t range = 0, first = 0, n = 0;   // the range the walk is in, the number of its first block, and its blocks
 
     __device__ __forceinline__ HeldView(const HeldKeys& h, int64_t item, int32_t D)
-        : ranges(h.ranges), codes(h.codes + item * 2 * h.capacity * D), exps(h.exps + item * 2 * (h.capacity / kBlock)),
+        : ranges(h.ranges), codes(h.codes + item * 2 * h.capacity * D), scales(h.scales + item * (h.capacity / kBlock)),
           capacity(h.capacity), total(h.blocks)
     {
+        n = (ranges.r[0].len + kBlock - 1) / kBlock;
+    }
+    __device__ __forceinline__ void restart(const HeldKeys& h, int64_t item, int32_t D)   // the same ranges of another item
+    {
+        codes = h.codes + item * 2 * h.capacity * D;
+        scales = h.scales + item * (h.capacity / kBlock);
+        range = first = 0;
         n = (ranges.r[0].len + kBlock - 1) / kBlock;
     }
     __device__ __forceinline__ int32_t blocks() const { return total; }
@@ -64,6 +83,12 @@ struct HeldView {
         walk(b);
         return min(ranges.r[range].len - (b - first) * kBlock, kBlock);
     }
+    __device__ __forceinline__ bool whole4(int32_t b)   // blocks b .. b + 3 are full, and of one range
+    {
+        if (b + 3 >= total) return false;
+        walk(b);
+        return b + 4 - first <= ranges.r[range].len / kBlock;
+    }
     __device__ __forceinline__ int32_t position(int32_t b)   // first slot of block b < total
     {
         walk(b);
@@ -71,46 +96,48 @@ struct HeldView {
     }
 };
 
-// Four e4m3 codes times a power of two, exactly, as bf16: the code's exponent and fraction are moved to their places (a bf16
-// 2^120 too small, which also holds for the codes without a leading one), then scaled twice, as 2^120 and the block's power of two
-// may be more than one bf16.
-__device__ __forceinline__ void widen4(uint32_t codes, __nv_bfloat162 scale, uint32_t& a, uint32_t& b)
+// The powers of two of a block's keys and values, in one word: the exponent fields of bf16 factors 2^(120 + e), or of 2^127 where
+// that is less, in bytes 0 (keys) and 1 (values), and what is then left of e in bytes 2 and 3.
+__device__ __forceinline__ uint32_t scale_word(int32_t ke, int32_t ve)
 {
-    constexpr uint32_t k2p120 = 0x7b807b80u;
-    const uint32_t c[2] = {__byte_perm(codes, 0u, 0x1404), __byte_perm(codes, 0u, 0x3424)};
-    uint32_t out[2];
+    return (uint32_t)(min(ke, 7) + 247) | (uint32_t)(min(ve, 7) + 247) << 8 | (uint32_t)max(ke - 7, 0) << 16 | (uint32_t)max(ve - 7, 0) << 24;
+}
+// 16 e4m3 codes times their power of two, exactly, as bf16.  With its sign spread over the byte above it a code is four bits short of
+// its place in a bf16 that is 2^120 too small (which also holds for codes without a leading one), so that a shift, a mask and a
+// product with the word's factor are all it takes; only magnitudes above 57 344 need a second product.
+__device__ __forceinline__ void widen16(const uint4& codes, uint32_t word, bool values, uint4& lo, uint4& hi)
+{
+    const uint32_t c[4] = {codes.x, codes.y, codes.z, codes.w};
+    const uint32_t f = ((values ? word >> 8 : word) & 0xffu) * 0x00800080u, left = (values ? word >> 24 : word >> 16) & 0xffu;
+    uint32_t out[8];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t w = ((c[i] >> 4) & 0x07f007f0u) | (c[i] & 0x80008000u);
-        const __nv_bfloat162 x = __hmul2(__hmul2(*reinterpret_cast<const __nv_bfloat162*>(&w), *reinterpret_cast<const __nv_bfloat162*>(&k2p120)), scale);
+    for (int i = 0; i < 8; ++i) {
+        uint32_t w;
+        if (i & 1) asm("prmt.b32 %0, %1, 0, 0xB3A2;" : "=r"(w) : "r"(c[i / 2]));
+        else asm("prmt.b32 %0, %1, 0, 0x9180;" : "=r"(w) : "r"(c[i / 2]));
+        w = (w << 4) & 0x87f087f0u;
+        const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&w), *reinterpret_cast<const __nv_bfloat162*>(&f));
         out[i] = *reinterpret_cast<const uint32_t*>(&x);
     }
-    a = out[0];
-    b = out[1];
-}
-__device__ __forceinline__ void widen16(const uint4& codes, __nv_bfloat162 scale, uint4& lo, uint4& hi)
-{
-    widen4(codes.x, scale, lo.x, lo.y);
-    widen4(codes.y, scale, lo.z, lo.w);
-    widen4(codes.z, scale, hi.x, hi.y);
-    widen4(codes.w, scale, hi.z, hi.w);
-}
-// 2^e for -126 <= e <= 127, twice
-__device__ __forceinline__ __nv_bfloat162 power_of_two(int32_t e)
-{
-    const uint32_t w = (uint32_t)(e + 127) * 0x00800080u;
-    return *reinterpret_cast<const __nv_bfloat162*>(&w);
-}
-__device__ __forceinline__ int32_t load_exponent(const int8_t* p)
-{
-    int32_t v;
-    asm volatile("ld.global.s8 %0, [%1];" : "=r"(v) : "l"(p));
-    return v;
+    if (left) {
+        const uint32_t f2 = (left + 127u) * 0x00800080u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&out[i]), *reinterpret_cast<const __nv_bfloat162*>(&f2));
+            out[i] = *reinterpret_cast<const uint32_t*>(&x);
+        }
+    }
+    lo = make_uint4(out[0], out[1], out[2], out[3]);
+    hi = make_uint4(out[4], out[5], out[6], out[7]);
 }
 // 16 bytes global -> shared, zeros where !real (src must be readable-looking but is not read then)
 __device__ __forceinline__ void copy16_or_zero(uint32_t dst, const void* src, bool real)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 #endif
 
