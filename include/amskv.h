@@ -302,7 +302,7 @@ AMSKV_API int amskv_read_segment(amskv_cache* cache, int layer, int segment, voi
  *   K, V      device pointers: [rows, kv_heads, keys, head_dim], of which row r has the first lengths[r]; or, with offsets, the
  *             keys of all rows one behind the other, [kv_heads, keys, head_dim], row r's from offsets[r] to offsets[r + 1] - 1.
  *             Strides (row, head, token) as in amskv_append, but that a row stride of 0 gives all rows the same keys; the
- *             row stride is not used with offsets.  A row's keys behind its last one are not read.
+ *             row stride is not used with offsets.  What lies behind a row's last key makes no difference, whatever it is.
  *   lengths   device pointer to rows int32, or NULL: all keys.
  *   offsets   device pointer to rows + 1 int32, or NULL.  (Lengths and offsets that point outside the tensor are cut to it.)
  *   max_keys  the most keys that a row has (0: `keys`); rows with more are cut to it.  It decides launch shapes: give the batch's

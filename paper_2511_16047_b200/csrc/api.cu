@@ -489,10 +489,11 @@ int amskv_attend(amskv_cache* cache, int layer, int scale, const void* Q, void* 
         const HeldRegion region = cache->held_region(layer);
         HeldKeys keys{region.codes, region.scales, region.capacity, 0, ranges};
         for (int i = 0; i < ranges.n; ++i) keys.blocks += (ranges.r[i].len + kBlock - 1) / kBlock;
+        e = cudaErrorNotSupported;
         if (takes_tiles(cache, T, 1, cache->heads, (int64_t)keys.blocks * kBlock))
             e = launch_attend_tiles(q, o, keys, T, cache->rows, cache->heads, cache->head_dim, cache->softmax_scale, cache->status_word(),
                                     cache->sm_count, static_cast<cudaStream_t>(stream));
-        else
+        if (e == cudaErrorNotSupported)   // (strides that no tensor map holds, too)
             e = launch_attend_rows(q, o, keys, T, cache->rows, cache->heads, cache->head_dim, cache->softmax_scale, cache->sm_count,
                                    static_cast<cudaStream_t>(stream));
         if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
@@ -821,13 +822,16 @@ int amskv_cross_attend(amskv_cache* cache, int scale, const amskv_encoder* enc, 
     if (rc != AMSKV_OK) return rc;
     if (cache->plan_only()) return AMSKV_ERR_UNSUPPORTED;
     const EncoderKeys keys{static_cast<const __nv_bfloat16*>(k.ptr), static_cast<const __nv_bfloat16*>(v.ptr), k.row, k.head, k.token,
-                           enc->lengths, enc->offsets, enc->keys, enc->max_keys > 0 ? std::min(enc->max_keys, enc->keys) : enc->keys};
+                           enc->lengths, enc->offsets, enc->keys, enc->max_keys > 0 ? std::min(enc->max_keys, enc->keys) : enc->keys,
+                           kv_rows == cache->rows && k.row != 0 && !enc->offsets};
     const int32_t group = cache->heads / enc->kv_heads;
-    const cudaError_t e = takes_tiles(cache, T, group, enc->kv_heads, keys.max_keys)
-        ? launch_attend_tiles(q, o, keys, T, cache->rows, enc->kv_heads, group, cache->head_dim, cache->softmax_scale, cache->status_word(),
-                              cache->sm_count, static_cast<cudaStream_t>(stream))
-        : launch_attend_rows(q, o, keys, T, cache->rows, enc->kv_heads, group, cache->head_dim, cache->softmax_scale, cache->sm_count,
-                             static_cast<cudaStream_t>(stream));
+    cudaError_t e = cudaErrorNotSupported;
+    if (takes_tiles(cache, T, group, enc->kv_heads, keys.max_keys))
+        e = launch_attend_tiles(q, o, keys, T, cache->rows, enc->kv_heads, group, cache->head_dim, cache->softmax_scale, cache->status_word(),
+                                cache->sm_count, static_cast<cudaStream_t>(stream));
+    if (e == cudaErrorNotSupported)   // (strides that no tensor map holds, too)
+        e = launch_attend_rows(q, o, keys, T, cache->rows, enc->kv_heads, group, cache->head_dim, cache->softmax_scale, cache->sm_count,
+                               static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
     return AMSKV_OK;
 }

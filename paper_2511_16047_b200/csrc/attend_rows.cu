@@ -163,11 +163,11 @@ attend_rows_kernel(const __nv_bfloat16* Q, int64_t q_row, int64_t q_head, int64_
         for (int i = 0; i < Pieces::kN; ++i) {
             const int r = w_row + i * Pieces::kRows;
             uint4 lo, hi;
-            widen16(next.k[i], next.scale[i], false, lo, hi);
+            widen16_by(next.k[i], next.scale[i], false, lo, hi);
             uint8_t* kt = st + r * C::kRowBytes;
             *reinterpret_cast<uint4*>(kt + (((2 * w_piece) ^ ((r & 1) << 2)) << 4)) = lo;
             *reinterpret_cast<uint4*>(kt + (((2 * w_piece + 1) ^ ((r & 1) << 2)) << 4)) = hi;
-            widen16(next.v[i], next.scale[i], true, lo, hi);
+            widen16_by(next.v[i], next.scale[i], true, lo, hi);
             uint8_t* vt = st + C::kTileBytes + r * C::kRowBytes;
             *reinterpret_cast<uint4*>(vt + (((2 * w_piece) ^ (r & 7)) << 4)) = lo;
             *reinterpret_cast<uint4*>(vt + (((2 * w_piece + 1) ^ (r & 7)) << 4)) = hi;

@@ -34,7 +34,7 @@ namespace {
 using namespace ptx;
 
 constexpr int kQRows = 128;       // query rows per tile = TMEM lanes
-constexpr int kQBoxRows = 32;     // query rows per bulk copy
+constexpr int kOutRows = 32;      // output rows per bulk copy: those of a warp
 constexpr int kKT = 64;           // keys per tile
 constexpr int kTileBlocks = kKT / kBlock;
 constexpr int kGroupWarps = 4;
@@ -49,8 +49,11 @@ struct TilesCfg {
     static constexpr bool kWide = D == 128;
     static constexpr int kCtasPerSm = kWide ? 1 : 2, kStages = kWide || kHeld ? 3 : 4;
     static constexpr int kSBufs = kWide ? 2 : 1, kQBufs = kWide && !kHeld ? 2 : 1;     // per stream
-    static constexpr int kMmaWarps = kWide ? 2 : 1, kLoadWarps = kWide ? 4 : 1;
-    static constexpr int kWarps = kMmaWarp + kMmaWarps + kLoadWarps, kThreads = kWarps * 32, kLoadThreads = kLoadWarps * 32;
+    // Outputs go through the place of their unit's queries (below): with one such place that holds the next unit's queries up, which with
+    // 64 channels costs more than scattered stores do.
+    static constexpr bool kBulkOut = kWide;
+    static constexpr int kMmaWarps = kWide ? 2 : 1, kLoadWarps = kWide && kHeld ? 4 : 1;
+    static constexpr int kWarps = kMmaWarp + kMmaWarps + kLoadWarps, kThreads = kWarps * 32;
     static constexpr int kHalves = D / 64;                      // 128-byte swizzle atoms per row
     static constexpr uint32_t kQBytes = kQRows * D * 2, kQHalfBytes = kQRows * 128;
     static constexpr uint32_t kKVBytes = kKT * D * 2, kKVHalfBytes = kKT * 128;
@@ -65,7 +68,7 @@ struct TilesCfg {
 };
 
 struct Barriers {
-    uint64_t q_full[2][2], kv_full[kMaxStages], kv_empty[kMaxStages], s_full[2][2], p_full[2][2], pv_done[2], o_full[2], drained[2];
+    uint64_t q_full[2][2], q_free[2][2], kv_full[kMaxStages], kv_empty[kMaxStages], s_full[2][2], p_full[2][2], pv_done[2], o_full[2], drained[2];
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -96,18 +99,20 @@ struct Unit {
     __device__ __forceinline__ int32_t qt(int g) const { return g ? qt1 : qt0; }
 };
 
-// Which 16-byte pieces of a tile a loading warp moves: of the tile's 128 rows, 64 of K and 64 of V behind them, the kRows of every
+// Which 16-byte pieces of a tile of codes a loading warp moves: of the tile's 128 rows, 64 of K and 64 of V behind them, the kRows of every
 // kLoadWarps-th pass, a row kPieces lanes wide.
-template <int D, bool kHeld>
-struct TileShare {
-    static constexpr int kPieces = kHeld ? D / 16 : D / 8, kRows = 32 / kPieces, kWarps = TilesCfg<D, kHeld>::kLoadWarps;
-    static constexpr int kN = 2 * kKT / kRows / kWarps;
-    static_assert(2 * kKT % (kRows * kWarps) == 0 && kBlock % (kRows * kWarps) == 0, "a block is whole rounds of the warps");
+template <int D>
+struct CodeShare {
+    static constexpr int kPieces = D / 16, kRows = 32 / kPieces, kWarps = TilesCfg<D, true>::kLoadWarps, kN = 2 * kKT / kRows / kWarps;
+    static constexpr int kBatch = 4;
+    static_assert(2 * kKT % (kRows * kWarps) == 0 && kBlock % (kRows * kWarps) == 0 && kN % kBatch == 0, "a block is whole rounds of the warps");
 };
 
 template <int D, bool kHeld>
 __global__ void __launch_bounds__(TilesCfg<D, kHeld>::kThreads, TilesCfg<D, kHeld>::kCtasPerSm)
-attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_bfloat16* O, int64_t o_row, int64_t o_head, int64_t o_tok,
+attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const __grid_constant__ CUtensorMap o_map, int3 opos,
+                    const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                    const __grid_constant__ CUtensorMap v_map16, int3 kpos, __nv_bfloat16* O, int64_t o_row, int64_t o_head, int64_t o_tok,
                     const __grid_constant__ EncoderKeys enc, const __grid_constant__ HeldKeys held, int32_t T,
                     const __grid_constant__ TilePlan plan, float scale_log2, int* status)
 {
@@ -128,6 +133,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
         for (int g = 0; g < 2; ++g) {
             for (int b = 0; b < 2; ++b) {
                 mbar_init(smem_u32(&bars->q_full[g][b]), 1);
+                mbar_init(smem_u32(&bars->q_free[g][b]), kGroupWarps);
                 mbar_init(smem_u32(&bars->s_full[g][b]), 1);
                 mbar_init(smem_u32(&bars->p_full[g][b]), kGroupWarps);
             }
@@ -136,16 +142,10 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
             mbar_init(smem_u32(&bars->drained[g]), 1);
         }
         for (int s = 0; s < C::kStages; ++s) {
-            mbar_init(smem_u32(&bars->kv_full[s]), kHeld ? C::kLoadWarps : C::kLoadThreads);
+            mbar_init(smem_u32(&bars->kv_full[s]), kHeld ? C::kLoadWarps : 33);   // (the lanes of the one loading warp, and its bulk copies)
             mbar_init(smem_u32(&bars->kv_empty[s]), C::kMmaWarps);   // one arrival per issuing warp, or two of the one whose tile it is
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    {
-        // query rows that a tile does not cover keep whatever the slot held before; start them at zero
-        uint4* qz = reinterpret_cast<uint4*>(smem_raw + (q_smem - raw));
-        for (uint32_t i = threadIdx.x; i < 2 * C::kQBufs * C::kQBytes / 16; i += C::kThreads) qz[i] = make_uint4(0, 0, 0, 0);
-        fence_async_smem();
     }
     if (warp == kMmaWarp) {
         __syncwarp();
@@ -180,62 +180,82 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
         // ------------------------------------------------------------ key/value stages
         uint32_t stage = 0, phase = 0;   // of the next tile
         bool ok = true;
-        // A stage is announced by its writers' arrivals alone; the fence that orders these writes before the tensor cores' reads is the
-        // issuing warps'.  Here it would wait for the loads and copies in flight, so that no tile could be fetched ahead: 10 521 keys of
-        // 128 channels 766 TF/s for CROSSTF, from 8 bits 261 for HELDTF.
-        auto announce = [&]() {
-            const uint32_t bar = kv_full0 + 8 * stage;
-            if (kHeld) {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar);
-            } else {   // once this thread's copies so far have landed
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-            }
+        auto next_stage = [&]() {
             if (++stage == C::kStages) {
                 stage = 0;
                 phase ^= 1u;
             }
         };
+        // What warps wrote themselves is announced by their arrivals alone; the fence that orders these writes before the tensor cores' reads
+        // is the issuing warps'.  Here it would wait for all copies in flight, so that no tile could be fetched ahead.
         auto free_stage = [&]() -> bool { return warp_wait(kv_empty0 + 8 * stage, phase ^ 1u, abort_flag); };
-        using Share = TileShare<D, kHeld>;
-        const int w = warp - load_warp, piece = lane % Share::kPieces, row = lane / Share::kPieces;   // row: of a pass
-        // Place of channels 8 c .. 8 c + 7 of a pass's row: what the lane gives, and what the pass does (its first row is a multiple of
-        // kRows, which divides 8, so that the two parts of the swizzle are apart).
-        auto lane_part = [&](int c) -> uint32_t { return (uint32_t)((c >> 3) * (int)C::kKVHalfBytes + row * 128 + (((c & 7) ^ row) << 4)); };
-        auto at_pass = [](uint32_t part, int p) -> uint32_t {
-            const int r = p * Share::kRows;
-            return (part ^ (uint32_t)((r & 7) << 4)) + (uint32_t)((r / kKT) * (int)C::kKVBytes + (r % kKT) * 128);
+        // place in a stage of channels 8 c .. 8 c + 7 of row r of its 128
+        auto place = [](int r, int c) -> uint32_t {
+            return (uint32_t)((r / kKT) * (int)C::kKVBytes + (c >> 3) * (int)C::kKVHalfBytes + (r % kKT) * 128 + (((c & 7) ^ (r & 7)) << 4));
         };
         if constexpr (!kHeld) {
-            const uint32_t part = lane_part(piece);
+            // Bulk copies, but for the last block of values of a row that it does not fill: these come piece by piece, with zeros behind the last
+            // one, as a probability of zero does not take away what a product makes of a NaN.  (Scores of keys behind the last one
+            // are overwritten, whatever they are.)
+            if (lane == 0) {
+                prefetch_tensormap(&k_map);
+                prefetch_tensormap(&v_map);
+                prefetch_tensormap(&v_map16);
+            }
+            constexpr int kPieces = D / 8, kRows = 32 / kPieces;
+            const int piece = lane % kPieces, row = lane / kPieces;
             EncoderBounds ahead = bounds_at(0);
             for (int32_t n = 0; ok && n < n_units; ++n) {
                 const Unit u = unit_at(n);
                 const EncoderView view(enc, u.row, u.head0 / plan.group, ahead);
+                const int32_t first_key = ahead.first(enc);
                 ahead = bounds_at(n + 1);
-                const int64_t to_b = (int64_t)(u.two ? u.head1 / plan.group - u.head0 / plan.group : 0) * enc.head;
+                const int32_t kv0 = u.head0 / plan.group, kv1 = u.two ? u.head1 / plan.group : kv0;
                 const int32_t blocks = view.blocks();
                 const int n_tiles = (blocks + kTileBlocks - 1) / kTileBlocks, per_tile = u.two && !u.shared ? 2 : 1;
                 for (int j = 0; ok && j < n_tiles; ++j) {
-                    const int rows = min(kTileBlocks, blocks - j * kTileBlocks) * kBlock;   // (the products read no others)
+                    const int32_t left = view.len - j * kKT;
                     for (int g = 0; g < per_tile; ++g) {
                         if (!free_stage()) {
                             ok = false;
                             break;
                         }
-                        const int64_t first = (int64_t)j * kKT * view.tok + (g ? to_b : 0);
-                        const __nv_bfloat16 *k0 = view.k + first + row * view.tok + piece * 8, *v0 = view.v + first + row * view.tok + piece * 8;
-                        const uint32_t dst = kv_smem + stage * C::kStageBytes;
-                        const int32_t left = view.len - j * kKT;
+                        const uint32_t dst = kv_smem + stage * C::kStageBytes, bar = kv_full0 + 8 * stage;
+                        const int whole = min(left / kBlock, kTileBlocks), over = left - whole * kBlock;   // blocks of values; values over (>= 16: none)
+                        if (elect_one()) {
+                            mbar_expect_tx(bar, C::kKVBytes + (uint32_t)whole * kBlock * D * 2);
+                            int c[4] = {0, 0, 0, 0};
+                            c[kpos.x] = first_key + j * kKT;
+                            c[kpos.y] = g ? kv1 : kv0;
+                            c[kpos.z] = enc.row_maps ? u.row : 0;
 #pragma unroll
-                        for (int i = 0; i < Share::kN; ++i) {
-                            const int p = w + i * Share::kWarps, r = p * Share::kRows % kKT;
-                            if (r >= rows) continue;
-                            const bool real = r + row < left;
-                            const __nv_bfloat16* src = p * Share::kRows >= kKT ? v0 : k0;
-                            copy16_or_zero(dst + at_pass(part, p), real ? src + r * view.tok : view.k, real);
+                            for (int h = 0; h < C::kHalves; ++h) tma_load_4d(dst + h * C::kKVHalfBytes, &k_map, bar, h * 64, c[1], c[2], c[3]);
+                            if (whole == kTileBlocks) {
+#pragma unroll
+                                for (int h = 0; h < C::kHalves; ++h)
+                                    tma_load_4d(dst + C::kKVBytes + h * C::kKVHalfBytes, &v_map, bar, h * 64, c[1], c[2], c[3]);
+                            } else {
+#pragma unroll 1
+                                for (int b = 0; b < whole; ++b, c[kpos.x] += kBlock)
+#pragma unroll
+                                    for (int h = 0; h < C::kHalves; ++h)
+                                        tma_load_4d(dst + C::kKVBytes + h * C::kKVHalfBytes + b * kBlock * 128, &v_map16, bar, h * 64, c[1], c[2], c[3]);
+                            }
                         }
-                        announce();
+                        __syncwarp();
+                        if (whole < kTileBlocks && over > 0) {
+                            const __nv_bfloat16* src = view.v + (int64_t)(j * kKT + whole * kBlock) * view.tok + (g ? (int64_t)(kv1 - kv0) * enc.head : 0) + piece * 8;
+#pragma unroll
+                            for (int i = 0; i < kBlock / kRows; ++i) {
+                                const int r = i * kRows + row;
+                                copy16_or_zero(dst + place(kKT + whole * kBlock + r, piece), r < over ? src + r * view.tok : view.v, r < over);
+                            }
+                            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");   // once they have landed
+                        } else {
+                            mbar_arrive(bar);
+                        }
+                        __syncwarp();
+                        next_stage();
                     }
                 }
             }
@@ -244,7 +264,17 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
             // Codes land in a ring of their own, each lane's where it will take them from again, and what belongs to the tile in 32 bytes of the
             // warp: the scale words of its four blocks and the slots that the products read (0: there is no further tile).  (With the
             // codes fetched into registers instead, a wait for a tile's waits for all younger ones too, as loads are counted, not named.)
-            const uint32_t part_lo = lane_part(2 * piece), part_hi = lane_part(2 * piece + 1);
+            using Share = CodeShare<D>;
+            // A lane's piece and row of a pass.  The row's lowest bit is bit 2 of the lane, so that eight lanes that store together, four pieces of two
+            // rows, meet all banks.
+            const int w = warp - load_warp, piece = (lane & 3) + (Share::kPieces == 8 ? (lane >> 1) & 4 : 0);
+            const int row = ((lane >> 2) & 1) + (Share::kPieces == 8 ? (lane >> 3) & 2 : (lane >> 2) & 6);
+            // (a pass's first row is a multiple of kRows, which divides 8, so that the swizzle of a row is that of the pass and that of the lane)
+            const uint32_t part_lo = place(row, 2 * piece), part_hi = place(row, 2 * piece + 1);
+            auto at_pass = [](uint32_t part, int p) -> uint32_t {
+                const int r = p * Share::kRows;
+                return (part ^ (uint32_t)((r & 7) << 4)) + (uint32_t)((r / kKT) * (int)C::kKVBytes + (r % kKT) * 128);
+            };
             const int n_tiles = (held.blocks + kTileBlocks - 1) / kTileBlocks;
             uint8_t* ring = smem_raw + (kv_smem - raw) + C::kStages * C::kStageBytes;
             const uint32_t ring_at = kv_smem + C::kStages * C::kStageBytes;
@@ -315,17 +345,39 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
                     break;
                 }
                 uint8_t* dst = smem_raw + (kv_smem - raw) + stage * C::kStageBytes;
-#pragma unroll
-                for (int i = 0; i < Share::kN; ++i) {
-                    const int b = i * Share::kWarps * Share::kRows % kKT / kBlock, p = w + i * Share::kWarps;
-                    if (b * kBlock >= rows) continue;
+                const uint8_t* mine = from + (w * 32 + lane) * 16;
+                auto put = [&](int i, const uint4& codes, uint32_t factor, uint32_t rest) {
+                    const int p = w + i * Share::kWarps;
                     uint4 lo, hi;
-                    widen16(*reinterpret_cast<const uint4*>(from + (p * 32 + lane) * 16), b == 0 ? words.x : b == 1 ? words.y : b == 2 ? words.z : words.w,
-                            i >= Share::kN / 2, lo, hi);
+                    widen16(codes, factor, rest, lo, hi);
                     *reinterpret_cast<uint4*>(dst + at_pass(part_lo, p)) = lo;
                     *reinterpret_cast<uint4*>(dst + at_pass(part_hi, p)) = hi;
+                };
+                auto codes_at = [&](int i) -> uint4 { return *reinterpret_cast<const uint4*>(mine + i * Share::kWarps * 512); };
+                if (rows == kKT && ((words.x | words.y | words.z | words.w) >> 16) == 0u) {
+                    // (nearly always) several passes' codes before the first is stored: no load can move above a store for the compiler
+#pragma unroll
+                    for (int i0 = 0; i0 < Share::kN; i0 += Share::kBatch) {
+                        uint4 x[Share::kBatch];
+#pragma unroll
+                        for (int i = 0; i < Share::kBatch; ++i) x[i] = codes_at(i0 + i);
+#pragma unroll
+                        for (int i = 0; i < Share::kBatch; ++i) {
+                            const int b = (i0 + i) * Share::kWarps * Share::kRows % kKT / kBlock;
+                            put(i0 + i, x[i], scale_factor(b == 0 ? words.x : b == 1 ? words.y : b == 2 ? words.z : words.w, i0 + i >= Share::kN / 2), 0u);
+                        }
+                    }
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < Share::kN; ++i) {
+                        const int b = i * Share::kWarps * Share::kRows % kKT / kBlock;
+                        const uint32_t v = b == 0 ? words.x : b == 1 ? words.y : b == 2 ? words.z : words.w;
+                        if (b * kBlock < rows) put(i, codes_at(i), scale_factor(v, i >= Share::kN / 2), scale_rest(v, i >= Share::kN / 2));
+                    }
                 }
-                announce();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(kv_full0 + 8 * stage);
+                next_stage();
                 slot = slot + 1 == C::kRing ? 0 : slot + 1;
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
@@ -398,7 +450,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
                     if (!s_first && j > 0 && !issue_pv(i, 0u)) goto stopped;
                     if (!(u.shared && i == 1)) {   // (one issuer: the second stream of a shared tile finds it landed)
                         if (!await(kv_full0 + 8 * stage, phase)) goto stopped;
-                        fence_async_smem();
+                        if (kHeld || j == n_tiles - 1) fence_async_smem();   // (a tile that warps wrote, or may have written a part of)
                     }
                     tc_fence_after();
                     const uint32_t buf = buf_of(t[i]);
@@ -426,25 +478,28 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
         const uint32_t lane_base = ((uint32_t)(wq * 32)) << 16;
         const uint32_t s_tmem0 = tmem + C::kSCol + g * C::kSBufs * kKT + lane_base, o_tmem = tmem + C::kOCol + g * D + lane_base;
         const bool q_loader = wq == 0 && lane == 0;
+        // the output rows start on 32-byte boundaries (the interface only promises 16)
         const bool o_sectors = ((reinterpret_cast<uintptr_t>(O) | (uintptr_t)(2 * o_row) | (uintptr_t)(2 * o_head) | (uintptr_t)(2 * o_tok)) & 31u) == 0;
         uint32_t q_asked = 0;     // query tiles requested
         int32_t q_next = 0;       // first unit not yet searched for one
+        const uint32_t q_free0 = smem_u32(&bars->q_free[0][0]);
+        // (one lane) the queries of the next unit not yet asked for, once the output that went through their place has left it
         auto load_next_q = [&]() {
             for (; q_next < n_units; ++q_next) {
                 const Unit u = unit_at(q_next);
                 if ((g == 1 && !u.two) || blocks_of(bounds_at(q_next)) == 0) continue;
-                const int32_t q0 = u.qt(g) * kQRows, boxes = (min(kQRows, T - q0) + kQBoxRows - 1) / kQBoxRows;
                 const uint32_t qb = qbuf_of(q_asked), bar = q_full0 + 16 * g + 8 * qb, dst = q_smem + (g * C::kQBufs + qb) * C::kQBytes;
-                mbar_expect_tx(bar, (uint32_t)boxes * kQBoxRows * D * 2);
+                if (C::kBulkOut && q_asked >= (uint32_t)C::kQBufs && !mbar_wait(q_free0 + 16 * g + 8 * qb, (q_asked / C::kQBufs - 1u) & 1u, abort_flag)) {
+                    report(status, kStatusSyncTimeout, abort_flag);
+                    return;
+                }
+                mbar_expect_tx(bar, C::kQBytes);
                 int c[4] = {0, 0, 0, 0};
+                c[qpos.x] = u.qt(g) * kQRows;
                 c[qpos.y] = u.head(g);
                 c[qpos.z] = u.row;
-                for (int bx = 0; bx < boxes; ++bx) {
-                    c[qpos.x] = q0 + bx * kQBoxRows;
 #pragma unroll
-                    for (int h = 0; h < C::kHalves; ++h)
-                        tma_load_4d(dst + h * C::kQHalfBytes + bx * kQBoxRows * 128, &q_map, bar, h * 64, c[1], c[2], c[3]);
-                }
+                for (int h = 0; h < C::kHalves; ++h) tma_load_4d(dst + h * C::kQHalfBytes, &q_map, bar, h * 64, c[1], c[2], c[3]);
                 ++q_asked;
                 ++q_next;
                 return;
@@ -452,11 +507,23 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
         };
         if (q_loader) {
             prefetch_tensormap(&q_map);
+            prefetch_tensormap(&o_map);
             for (int i = 0; i < C::kQBufs; ++i) load_next_q();
         }
         __syncwarp();
         uint32_t t = 0, un = 0;   // tiles and units of this stream
-        bool ok = true;
+        bool ok = true, to_release = false;
+        auto release_q = [&]() {   // the output of the last unit has left the place of its queries; the next ones are asked for
+            if (to_release) {
+                if (lane == 0) {
+                    bulk_wait_read<0>();
+                    mbar_arrive(q_free0 + 16 * g + 8 * qbuf_of(C::kQBufs == 2 ? un + 1u : 0u));
+                }
+                if (q_loader) load_next_q();
+                __syncwarp();
+                to_release = false;
+            }
+        };
         EncoderBounds ahead = bounds_at(0);
         for (int32_t n = 0; ok && n < n_units; ++n) {
             const Unit u = unit_at(n);
@@ -476,7 +543,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
                     break;
                 }
                 tc_fence_after();
-                if (j == n_tiles - 1 && q_loader) load_next_q();   // the last S has landed: its queries are no longer read
+                if (!C::kBulkOut && j == n_tiles - 1 && q_loader) load_next_q();   // the last S has landed: its queries are no longer read
                 if (warp_live) {
                     const int groups = min(kTileBlocks, blocks - j * kTileBlocks);
                     uint64_t keep = ~0ull;   // a bit per column that holds a key
@@ -579,6 +646,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full0 + 16 * g + 8 * buf);
+                if (C::kBulkOut && C::kQBufs == 2 && j == 0) release_q();   // (of the unit before)
             }
             if (!ok) break;
             if (n_tiles > 0) {
@@ -590,18 +658,13 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
                 ++un;
                 tc_fence_after();
             }
-            if (warp_live) {
-                const float inv = n_tiles > 0 ? 1.f / l : 0.f;
+            if (!C::kBulkOut && warp_live && n_tiles > 0) {
+                const float inv = 1.f / l;
                 __nv_bfloat16* dst = O + u.row * o_row + u.head(g) * o_head + (int64_t)(u.qt(g) * kQRows + r) * o_tok;
 #pragma unroll
                 for (int cb = 0; cb < D / 32; ++cb) {
                     uint32_t o[32];
-                    if (n_tiles > 0) {
-                        tmem_ld32(o_tmem + cb * 32, o);
-                    } else {   // a row without keys: zeros
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = 0u;
-                    }
+                    tmem_ld32(o_tmem + cb * 32, o);
                     if (r < valid_rows) {
                         uint32_t w[16];
 #pragma unroll
@@ -619,10 +682,51 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, __nv_b
                         }
                     }
                 }
+            } else if (warp_live && n_tiles > 0) {
+                // Through the place of the unit's queries, which nobody reads any more, and out as one bulk copy per 64 channels: stores straight
+                // from the registers, a row per thread, take a memory transaction for every 32 bytes.  Rows past T are outside the tensor.
+                const float inv = 1.f / l;
+                const uint32_t place = q_smem + (g * C::kQBufs + qbuf_of(un - 1u)) * C::kQBytes + wq * 32 * 128;
+                uint8_t* mine = smem_raw + (place - raw) + lane * 128;
+#pragma unroll
+                for (int cb = 0; cb < D / 32; ++cb) {
+                    uint32_t o[32];
+                    tmem_ld32(o_tmem + cb * 32, o);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(o[8 * c + 2 * i]) * inv, __uint_as_float(o[8 * c + 2 * i + 1]) * inv);
+                            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+                        }
+                        *reinterpret_cast<uint4*>(mine + (cb >> 1) * C::kQHalfBytes + ((((cb & 1) * 4 + c) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    int c[4] = {0, 0, 0, 0};
+                    c[opos.x] = u.qt(g) * kQRows + wq * 32;
+                    c[opos.y] = u.head(g);
+                    c[opos.z] = u.row;
+#pragma unroll
+                    for (int h = 0; h < C::kHalves; ++h) tma_store_4d(&o_map, place + h * C::kQHalfBytes, h * 64, c[1], c[2], c[3]);
+                    bulk_commit();
+                }
+            } else if (warp_live && r < valid_rows) {   // a row without keys: zeros
+                uint4* dst = reinterpret_cast<uint4*>(O + u.row * o_row + u.head(g) * o_head + (int64_t)(u.qt(g) * kQRows + r) * o_tok);
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) dst[c] = make_uint4(0, 0, 0, 0);
+            }
+            if (C::kBulkOut && n_tiles > 0) {
+                to_release = true;
+                if (C::kQBufs == 1) release_q();
             }
             tc_fence_before();   // the reads of O come before the arrival on p_full for the next unit's first tile
         }
-        // query tiles requested but never used must land before the CTA ends
+        if (lane == 0) bulk_wait_all();   // the output is written before the CTA ends
+        // query tiles requested but never used must land before that, too
         if (q_loader)
             for (uint32_t q = un; q < q_asked; ++q)
                 for (uint32_t i = 0; i < kSpinLimit; ++i)
@@ -666,13 +770,27 @@ cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, c
     plan.units = rows * plan.units_per_row;
     CUtensorMap qm;
     int pos[3];
-    if (!tc_encode_q_map(Q, T, rows, plan.heads, D, kQBoxRows, &qm, pos)) return cudaErrorNotSupported;
+    if (!tc_encode_q_map(Q, T, rows, plan.heads, D, kQRows, &qm, pos)) return cudaErrorNotSupported;
+    CUtensorMap om, km, vm, vm16;
+    int opos[3], kpos[3] = {1, 2, 3}, vpos[3] = {1, 2, 3};
+    if (!tc_encode_q_map(O, T, rows, plan.heads, D, kOutRows, &om, opos)) return cudaErrorNotSupported;
+    memset(&km, 0, sizeof(km));
+    memset(&vm, 0, sizeof(vm));
+    memset(&vm16, 0, sizeof(vm16));
+    if (!kHeld) {
+        const int32_t kv_rows = enc.row_maps ? rows : 1;
+        if (!tc_encode_q_map(Strided{enc.K, enc.row, enc.head, enc.tok}, enc.keys, kv_rows, kv_heads, D, kKT, &km, kpos) ||
+            !tc_encode_q_map(Strided{enc.V, enc.row, enc.head, enc.tok}, enc.keys, kv_rows, kv_heads, D, kKT, &vm, vpos) ||
+            !tc_encode_q_map(Strided{enc.V, enc.row, enc.head, enc.tok}, enc.keys, kv_rows, kv_heads, D, kBlock, &vm16, vpos))
+            return cudaErrorNotSupported;
+    }
     static SharedMemoryOptIn opt_in;
     const cudaError_t oe = opt_in.ensure(attend_tiles_kernel<D, kHeld>, (int)C::kSmemBytes);
     if (oe != cudaSuccess) return oe;
     const int64_t grid = std::min<int64_t>(plan.units, (int64_t)sm_count * C::kCtasPerSm);
     return launch_kernel(true, attend_tiles_kernel<D, kHeld>, dim3((unsigned)grid), dim3(C::kThreads), KernelMemory(C::kSmemBytes), stream, qm,
-                         make_int3(pos[0], pos[1], pos[2]), (__nv_bfloat16*)O.ptr, O.row, O.head, O.token, enc, held, T, plan,
+                         make_int3(pos[0], pos[1], pos[2]), om, make_int3(opos[0], opos[1], opos[2]), km, vm, vm16, make_int3(kpos[0], kpos[1], kpos[2]),
+                         (__nv_bfloat16*)O.ptr, O.row, O.head, O.token, enc, held, T, plan,
                          softmax_scale * 1.4426950408889634f, status);
 }
 

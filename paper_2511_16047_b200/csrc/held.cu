@@ -97,7 +97,7 @@ read_segment_kernel(const void* region, const uint32_t* scales, int32_t capacity
         uint4* dst = reinterpret_cast<uint4*>((kv ? V : K) + row * row_stride + head * head_stride + tok * tok_stride + piece * kValues);
         if (kHeld) {
             uint4 lo, hi;
-            widen16(x, load_word(scales + item * (capacity / kBlock) + (offset + tok) / kBlock), kv != 0, lo, hi);
+            widen16_by(x, load_word(scales + item * (capacity / kBlock) + (offset + tok) / kBlock), kv != 0, lo, hi);
             dst[0] = lo;
             dst[1] = hi;
         } else {

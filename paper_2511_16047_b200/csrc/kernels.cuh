@@ -182,6 +182,7 @@ struct EncoderKeys {
     int64_t row, head, tok;      // element strides, the same for K and V
     const int32_t *lengths, *offsets;
     int32_t keys, max_keys;      // extent of the tensor; the most that a row has
+    bool row_maps;               // rows have keys of their own (not packed, and not the same for all)
 };
 // A layer's region held in 8 bits: item i owns 2 * capacity * D codes, keys first, and capacity / 16 words with the powers of two of
 // a block's keys and values.

@@ -102,13 +102,15 @@ __device__ __forceinline__ uint32_t scale_word(int32_t ke, int32_t ve)
 {
     return (uint32_t)(min(ke, 7) + 247) | (uint32_t)(min(ve, 7) + 247) << 8 | (uint32_t)max(ke - 7, 0) << 16 | (uint32_t)max(ve - 7, 0) << 24;
 }
+// of a word, for keys or values: the factor twice, and what is left of e
+__device__ __forceinline__ uint32_t scale_factor(uint32_t word, bool values) { return ((values ? word >> 8 : word) & 0xffu) * 0x00800080u; }
+__device__ __forceinline__ uint32_t scale_rest(uint32_t word, bool values) { return (values ? word >> 24 : word >> 16) & 0xffu; }
 // 16 e4m3 codes times their power of two, exactly, as bf16.  With its sign spread over the byte above it a code is four bits short of
 // its place in a bf16 that is 2^120 too small (which also holds for codes without a leading one), so that a shift, a mask and a
 // product with the word's factor are all it takes; only magnitudes above 57 344 need a second product.
-__device__ __forceinline__ void widen16(const uint4& codes, uint32_t word, bool values, uint4& lo, uint4& hi)
+__device__ __forceinline__ void widen16(const uint4& codes, uint32_t f, uint32_t left, uint4& lo, uint4& hi)
 {
     const uint32_t c[4] = {codes.x, codes.y, codes.z, codes.w};
-    const uint32_t f = ((values ? word >> 8 : word) & 0xffu) * 0x00800080u, left = (values ? word >> 24 : word >> 16) & 0xffu;
     uint32_t out[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -129,6 +131,10 @@ __device__ __forceinline__ void widen16(const uint4& codes, uint32_t word, bool 
     }
     lo = make_uint4(out[0], out[1], out[2], out[3]);
     hi = make_uint4(out[4], out[5], out[6], out[7]);
+}
+__device__ __forceinline__ void widen16_by(const uint4& codes, uint32_t word, bool values, uint4& lo, uint4& hi)
+{
+    widen16(codes, scale_factor(word, values), scale_rest(word, values), lo, hi);
 }
 // 16 bytes global -> shared, zeros where !real (src must be readable-looking but is not read then)
 __device__ __forceinline__ void copy16_or_zero(uint32_t dst, const void* src, bool real)
