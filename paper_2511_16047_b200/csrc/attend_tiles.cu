@@ -42,13 +42,16 @@ constexpr int kMmaWarp = 8;
 constexpr int kMaxStages = 4;
 constexpr float kRescaleLog2 = 8.f;
 constexpr float kSumLimit = 1.8446744e19f;   // 2^64
-constexpr int kPolyEvery = 6;     // every 6th pair of exponentials from the FMA pipe, as in the paired kernel
+constexpr int kMaskTab = 192;                // tiles of a cache whose masks are tabulated in shared memory
 
 template <int D, bool kHeld>
 struct TilesCfg {
     static constexpr bool kWide = D == 128;
     static constexpr int kCtasPerSm = kWide ? 1 : 2, kStages = kWide || kHeld ? 3 : 4;
     static constexpr int kSBufs = kWide ? 2 : 1, kQBufs = kWide && !kHeld ? 2 : 1;     // per stream
+    // Every so many pairs of exponentials come from the FMA pipe (0: none), where the special-function unit is what a tile waits for.  Not
+    // beside warps that widen codes with two CTAs' softmax warps, which leave no room for more instructions.
+    static constexpr int kPolyEvery = kWide ? 6 : kHeld ? 0 : 12;
     // Outputs go through the place of their unit's queries (below): with one such place that holds the next unit's queries up, which with
     // 64 channels costs more than scattered stores do.
     static constexpr bool kBulkOut = kWide;
@@ -60,7 +63,8 @@ struct TilesCfg {
     static constexpr uint32_t kStageBytes = 2 * kKVBytes;
     static constexpr int kRing = kHeld ? 3 : 0;                 // tiles of codes on their way, each with 32 bytes per warp behind it
     static constexpr uint32_t kCodeBytes = 2 * kKT * D, kRingBytes = kCodeBytes + kLoadWarps * 32;
-    static constexpr uint32_t kSmemBytes = 2048 + 2 * kQBufs * kQBytes + kStages * kStageBytes + kRing * kRingBytes;   // barriers and slack in front
+    static constexpr uint32_t kSmemBytes = 2048 + 2 * kQBufs * kQBytes + kStages * kStageBytes + kRing * kRingBytes +
+                                           (kHeld ? kMaskTab * 8 : 0);   // barriers and slack in front
     static constexpr uint32_t kTmemCols = kWide ? 512 : 256, kSCol = 0, kOCol = 2 * kSBufs * kKT;   // S of both streams, then O of both
     static_assert(kOCol + 2 * D <= kTmemCols && kCtasPerSm * kTmemCols <= 512, "tensor memory");
     static_assert(kCtasPerSm * (kSmemBytes + 1024) <= 228 * 1024, "shared memory");
@@ -146,6 +150,20 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             mbar_init(smem_u32(&bars->kv_empty[s]), C::kMmaWarps);   // one arrival per issuing warp, or two of the one whose tile it is
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    // Of a cache's tiles, the same for all units: a bit per slot that holds a key.  (Worked out tile by tile the softmax warps would pay for it:
+    // 430 keys x 256 queries x 3 840 heads of 64 311 us, 246 without.)
+    auto mask_of = [](HeldView& view, int j) -> uint64_t {
+        if (view.whole4(j * kTileBlocks)) return ~0ull;
+        uint64_t keep = 0;
+#pragma unroll
+        for (int b = 0; b < kTileBlocks; ++b) keep |= ((1ull << view.valid(j * kTileBlocks + b)) - 1ull) << (b * kBlock);
+        return keep;
+    };
+    uint64_t* mask_tab = reinterpret_cast<uint64_t*>(smem_raw + (kv_smem - raw) + C::kStages * C::kStageBytes + C::kRing * C::kRingBytes);
+    if (kHeld) {
+        HeldView view(held, 0, D);
+        for (int j = threadIdx.x; j < kMaskTab && j * kTileBlocks < held.blocks; j += C::kThreads) mask_tab[j] = mask_of(view, j);
     }
     if (warp == kMmaWarp) {
         __syncwarp();
@@ -251,8 +269,8 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                                 copy16_or_zero(dst + place(kKT + whole * kBlock + r, piece), r < over ? src + r * view.tok : view.v, r < over);
                             }
                             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");   // once they have landed
-                        } else {
-                            mbar_arrive(bar);
+                        } else if (lane == 0) {
+                            mbar_arrive_n(bar, 32);
                         }
                         __syncwarp();
                         next_stage();
@@ -530,7 +548,6 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             const int32_t len = ahead.len(enc), blocks = blocks_of(ahead);
             ahead = bounds_at(n + 1);
             if (g == 1 && !u.two) continue;
-            HeldView hv(held, 0, D);
             const int n_tiles = (blocks + kTileBlocks - 1) / kTileBlocks;
             const int32_t valid_rows = min(kQRows, T - u.qt(g) * kQRows);
             const bool warp_live = wq * 32 < valid_rows;
@@ -548,10 +565,11 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     const int groups = min(kTileBlocks, blocks - j * kTileBlocks);
                     uint64_t keep = ~0ull;   // a bit per column that holds a key
                     if (kHeld) {
-                        if (!hv.whole4(j * kTileBlocks)) {
-                            keep = 0;
-#pragma unroll
-                            for (int b = 0; b < kTileBlocks; ++b) keep |= ((1ull << hv.valid(j * kTileBlocks + b)) - 1ull) << (b * kBlock);
+                        if (j < kMaskTab) {
+                            keep = mask_tab[j];
+                        } else {
+                            HeldView view(held, 0, D);
+                            keep = mask_of(view, j);
                         }
                     } else if (len - j * kKT < kKT) {
                         keep = (1ull << (len - j * kKT)) - 1ull;
@@ -582,8 +600,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     }
                     // P over S, bf16 (the type of V) for the product; the sums take the probabilities as they are.  Blocks behind the last one
                     // are not read by the product and keep stale bits.
-                    float tile_sum;
-                    for (bool again = false;; again = true) {
+                    auto exp_tile = [&]() -> float {
                         float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
                         for (int grp = 0; grp < kTileBlocks; ++grp) {
@@ -591,10 +608,10 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                                 uint32_t pk[8];
 #pragma unroll
                                 for (int ii = 0; ii < 8; ++ii) {
-                                    const int i = (grp & 1) * 8 + ii, c = grp * 16 + 2 * ii;
+                                    const int i = grp * 8 + ii, c = 2 * i;
                                     float x0, x1, p0, p1;
                                     fma2(x0, x1, __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]), scale_log2, scale_log2, nb, nb);
-                                    if (i % kPolyEvery == 0) {
+                                    if (C::kPolyEvery > 0 && i % (C::kPolyEvery > 0 ? C::kPolyEvery : 1) == 0) {
                                         exp2_poly2(p0, p1, x0, x1);
                                     } else {
                                         p0 = fast_exp2(x0);
@@ -607,39 +624,43 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                                 tmem_st8_nowait(s_tmem + grp * 8, pk);
                             }
                         }
-                        tile_sum = sum0 + sum1;
+                        return sum0 + sum1;
+                    };
+                    float tile_sum = exp_tile();
+                    if (j > 0) {
                         // (the polynomial ends at 2^126, so that it cannot hide a row that has outgrown its reference)
-                        const bool over = j > 0 && !(tile_sum <= kSumLimit);
-                        if (again || !__any_sync(0xffffffffu, over)) break;
-                        // Rare.  The P V before must be done: with one S buffer it was issued before this S, whose arrival covers it; with two it
-                        // has an arrival of its own (the next one needs the P that this tile has not announced yet).
-                        if (C::kSBufs == 2) {
-                            if (!__all_sync(0xffffffffu, mbar_wait(pv_done0 + 8 * g, (t - 1u) & 1u, abort_flag))) {
-                                report(status, kStatusSyncTimeout, abort_flag);
-                                ok = false;
-                                break;
+                        const bool over = !(tile_sum <= kSumLimit);
+                        if (__any_sync(0xffffffffu, over)) {
+                            // Rare.  The P V before must be done: with one S buffer it was issued before this S, whose arrival covers it; with two it
+                            // has an arrival of its own (the next one needs the P that this tile has not announced yet).
+                            if (C::kSBufs == 2) {
+                                if (!__all_sync(0xffffffffu, mbar_wait(pv_done0 + 8 * g, (t - 1u) & 1u, abort_flag))) {
+                                    report(status, kStatusSyncTimeout, abort_flag);
+                                    ok = false;
+                                    break;
+                                }
+                                tc_fence_after();
                             }
-                            tc_fence_after();
-                        }
-                        tmem_wait_st();
-                        const float mt = tile_max();
-                        float alpha = 1.f;
-                        if (over || fmaf(mt, scale_log2, nb) > kRescaleLog2) {
-                            alpha = fast_exp2((m_ref - mt) * scale_log2);
-                            m_ref = mt;
-                            nb = -mt * scale_log2;
-                            l *= alpha;
-                        }
+                            tmem_wait_st();
+                            const float mt = tile_max();
+                            float alpha = 1.f;
+                            if (over || fmaf(mt, scale_log2, nb) > kRescaleLog2) {
+                                alpha = fast_exp2((m_ref - mt) * scale_log2);
+                                m_ref = mt;
+                                nb = -mt * scale_log2;
+                                l *= alpha;
+                            }
 #pragma unroll 1
-                        for (int cb = 0; cb < D / 8; ++cb) {
-                            uint32_t o[8];
-                            tmem_ld8(o_tmem + cb * 8, o);
+                            for (int cb = 0; cb < D / 8; ++cb) {
+                                uint32_t o[8];
+                                tmem_ld8(o_tmem + cb * 8, o);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                            tmem_st8(o_tmem + cb * 8, o);
+                                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                tmem_st8(o_tmem + cb * 8, o);
+                            }
+                            tile_sum = exp_tile();
                         }
                     }
-                    if (!ok) break;
                     l += tile_sum;
                     tmem_wait_st();
                 }
