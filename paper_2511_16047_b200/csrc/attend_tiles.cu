@@ -57,6 +57,7 @@ struct TilesCfg {
     static constexpr bool kBulkOut = kWide;
     static constexpr int kMmaWarps = kWide ? 2 : 1, kLoadWarps = kWide && kHeld ? 4 : 1;
     static constexpr int kWarps = kMmaWarp + kMmaWarps + kLoadWarps, kThreads = kWarps * 32;
+    static constexpr bool kLoaderQ = kQBufs == 2;               // the loading warp fetches the queries, else a lane of each softmax group does
     static constexpr int kHalves = D / 64;                      // 128-byte swizzle atoms per row
     static constexpr uint32_t kQBytes = kQRows * D * 2, kQHalfBytes = kQRows * 128;
     static constexpr uint32_t kKVBytes = kKT * D * 2, kKVHalfBytes = kKT * 128;
@@ -111,6 +112,13 @@ struct CodeShare {
     static constexpr int kBatch = 4;
     static_assert(2 * kKT % (kRows * kWarps) == 0 && kBlock % (kRows * kWarps) == 0 && kN % kBatch == 0, "a block is whole rounds of the warps");
 };
+
+// Coordinates 1 to 3 of a rank-4 map whose token, head and row dimensions are at `pos`.
+__device__ __forceinline__ int3 coords(const int3& pos, int tok, int head, int row)
+{
+    auto at = [&](int i) { return pos.x == i ? tok : pos.y == i ? head : row; };
+    return make_int3(at(1), at(2), at(3));
+}
 
 template <int D, bool kHeld>
 __global__ void __launch_bounds__(TilesCfg<D, kHeld>::kThreads, TilesCfg<D, kHeld>::kCtasPerSm)
@@ -194,6 +202,24 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
     // blocks of keys of a row; a row without any is left out by every role (but for the zeros it gets)
     auto blocks_of = [&](const EncoderBounds& b) -> int32_t { return kHeld ? held.blocks : (b.len(enc) + kBlock - 1) / kBlock; };
 
+    const uint32_t q_free0 = smem_u32(&bars->q_free[0][0]);
+    // (one lane) the query tile of stream g in unit u, the q-th of the stream
+    auto load_q = [&](const Unit& u, int g, uint32_t q) {
+        const uint32_t qb = qbuf_of(q), bar = q_full0 + 16 * g + 8 * qb, dst = q_smem + (g * C::kQBufs + qb) * C::kQBytes;
+        mbar_expect_tx(bar, C::kQBytes);
+        const int3 c = coords(qpos, u.qt(g) * kQRows, u.head(g), u.row);
+#pragma unroll
+        for (int h = 0; h < C::kHalves; ++h) tma_load_4d(dst + h * C::kQHalfBytes, &q_map, bar, h * 64, c.x, c.y, c.z);
+    };
+    // the output that went through the place of query tile q has left it
+    auto q_place_free = [&](int g, uint32_t q) -> bool {
+        return q < (uint32_t)C::kQBufs || mbar_wait(q_free0 + 16 * g + 8 * qbuf_of(q), (q / C::kQBufs - 1u) & 1u, abort_flag);
+    };
+    auto await_q = [&](int g, uint32_t q) {   // whatever becomes of the launch, a copy into shared memory ends before the CTA does
+        for (uint32_t i = 0; i < kSpinLimit; ++i)
+            if (mbar_try_wait(q_full0 + 16 * g + 8 * qbuf_of(q), qpar_of(q))) break;
+    };
+
     if (warp >= load_warp && warp < load_warp + C::kLoadWarps) {
         // ------------------------------------------------------------ key/value stages
         uint32_t stage = 0, phase = 0;   // of the next tile
@@ -222,6 +248,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             }
             constexpr int kPieces = D / 8, kRows = 32 / kPieces;
             const int piece = lane % kPieces, row = lane / kPieces;
+            uint32_t q_asked[2] = {0, 0}, issued = 0;
             EncoderBounds ahead = bounds_at(0);
             for (int32_t n = 0; ok && n < n_units; ++n) {
                 const Unit u = unit_at(n);
@@ -231,6 +258,19 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                 const int32_t kv0 = u.head0 / plan.group, kv1 = u.two ? u.head1 / plan.group : kv0;
                 const int32_t blocks = view.blocks();
                 const int n_tiles = (blocks + kTileBlocks - 1) / kTileBlocks, per_tile = u.two && !u.shared ? 2 : 1;
+                if (C::kLoaderQ && n_tiles > 0) {
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        if (g == 1 && !u.two) break;
+                        if (!__all_sync(0xffffffffu, q_place_free(g, q_asked[g]))) {
+                            ok = false;
+                            break;
+                        }
+                        if (elect_one()) load_q(u, g, q_asked[g]);
+                        __syncwarp();
+                        ++q_asked[g];
+                    }
+                }
                 for (int j = 0; ok && j < n_tiles; ++j) {
                     const int32_t left = view.len - j * kKT;
                     for (int g = 0; g < per_tile; ++g) {
@@ -242,22 +282,22 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                         const int whole = min(left / kBlock, kTileBlocks), over = left - whole * kBlock;   // blocks of values; values over (>= 16: none)
                         if (elect_one()) {
                             mbar_expect_tx(bar, C::kKVBytes + (uint32_t)whole * kBlock * D * 2);
-                            int c[4] = {0, 0, 0, 0};
-                            c[kpos.x] = first_key + j * kKT;
-                            c[kpos.y] = g ? kv1 : kv0;
-                            c[kpos.z] = enc.row_maps ? u.row : 0;
+                            const int tok = first_key + j * kKT, head = g ? kv1 : kv0, from = enc.row_maps ? u.row : 0;
+                            const int3 c = coords(kpos, tok, head, from);
 #pragma unroll
-                            for (int h = 0; h < C::kHalves; ++h) tma_load_4d(dst + h * C::kKVHalfBytes, &k_map, bar, h * 64, c[1], c[2], c[3]);
+                            for (int h = 0; h < C::kHalves; ++h) tma_load_4d(dst + h * C::kKVHalfBytes, &k_map, bar, h * 64, c.x, c.y, c.z);
                             if (whole == kTileBlocks) {
 #pragma unroll
                                 for (int h = 0; h < C::kHalves; ++h)
-                                    tma_load_4d(dst + C::kKVBytes + h * C::kKVHalfBytes, &v_map, bar, h * 64, c[1], c[2], c[3]);
+                                    tma_load_4d(dst + C::kKVBytes + h * C::kKVHalfBytes, &v_map, bar, h * 64, c.x, c.y, c.z);
                             } else {
 #pragma unroll 1
-                                for (int b = 0; b < whole; ++b, c[kpos.x] += kBlock)
+                                for (int b = 0; b < whole; ++b) {
+                                    const int3 cb = coords(kpos, tok + b * kBlock, head, from);
 #pragma unroll
                                     for (int h = 0; h < C::kHalves; ++h)
-                                        tma_load_4d(dst + C::kKVBytes + h * C::kKVHalfBytes + b * kBlock * 128, &v_map16, bar, h * 64, c[1], c[2], c[3]);
+                                        tma_load_4d(dst + C::kKVBytes + h * C::kKVHalfBytes + b * kBlock * 128, &v_map16, bar, h * 64, cb.x, cb.y, cb.z);
+                                }
                             }
                         }
                         __syncwarp();
@@ -273,11 +313,21 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                             mbar_arrive_n(bar, 32);
                         }
                         __syncwarp();
+                        ++issued;
                         next_stage();
                     }
                 }
             }
+            // whatever becomes of the launch, copies into shared memory end before the CTA does
             asm volatile("cp.async.wait_all;" ::: "memory");
+            for (uint32_t q = issued > (uint32_t)C::kStages ? issued - C::kStages : 0u; q < issued; ++q)
+                for (uint32_t i = 0; i < kSpinLimit; ++i)
+                    if (mbar_try_wait(kv_full0 + 8 * (q % C::kStages), (q / C::kStages) & 1u)) break;
+            if (C::kLoaderQ) {
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+                    for (uint32_t q = q_asked[g] > 2u ? q_asked[g] - 2u : 0u; q < q_asked[g]; ++q) await_q(g, q);
+            }
         } else {
             // Codes land in a ring of their own, each lane's where it will take them from again, and what belongs to the tile in 32 bytes of the
             // warp: the scale words of its four blocks and the slots that the products read (0: there is no further tile).  (With the
@@ -500,49 +550,45 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
         const bool o_sectors = ((reinterpret_cast<uintptr_t>(O) | (uintptr_t)(2 * o_row) | (uintptr_t)(2 * o_head) | (uintptr_t)(2 * o_tok)) & 31u) == 0;
         uint32_t q_asked = 0;     // query tiles requested
         int32_t q_next = 0;       // first unit not yet searched for one
-        const uint32_t q_free0 = smem_u32(&bars->q_free[0][0]);
-        // (one lane) the queries of the next unit not yet asked for, once the output that went through their place has left it
-        auto load_next_q = [&]() {
-            for (; q_next < n_units; ++q_next) {
+        // (one lane) the queries of the first unit from q_next on that has any; `at_next` is what is known of unit q_next's row
+        auto load_next_q = [&](EncoderBounds at_next) {
+            while (q_next < n_units) {
                 const Unit u = unit_at(q_next);
-                if ((g == 1 && !u.two) || blocks_of(bounds_at(q_next)) == 0) continue;
-                const uint32_t qb = qbuf_of(q_asked), bar = q_full0 + 16 * g + 8 * qb, dst = q_smem + (g * C::kQBufs + qb) * C::kQBytes;
-                if (C::kBulkOut && q_asked >= (uint32_t)C::kQBufs && !mbar_wait(q_free0 + 16 * g + 8 * qb, (q_asked / C::kQBufs - 1u) & 1u, abort_flag)) {
+                const bool none = (g == 1 && !u.two) || blocks_of(at_next) == 0;
+                ++q_next;
+                if (none) {
+                    at_next = bounds_at(q_next);
+                    continue;
+                }
+                if (C::kBulkOut && !q_place_free(g, q_asked)) {
                     report(status, kStatusSyncTimeout, abort_flag);
                     return;
                 }
-                mbar_expect_tx(bar, C::kQBytes);
-                int c[4] = {0, 0, 0, 0};
-                c[qpos.x] = u.qt(g) * kQRows;
-                c[qpos.y] = u.head(g);
-                c[qpos.z] = u.row;
-#pragma unroll
-                for (int h = 0; h < C::kHalves; ++h) tma_load_4d(dst + h * C::kQHalfBytes, &q_map, bar, h * 64, c[1], c[2], c[3]);
+                load_q(u, g, q_asked);
                 ++q_asked;
-                ++q_next;
                 return;
             }
         };
         if (q_loader) {
             prefetch_tensormap(&q_map);
             prefetch_tensormap(&o_map);
-            for (int i = 0; i < C::kQBufs; ++i) load_next_q();
+            if (!C::kLoaderQ) load_next_q(bounds_at(0));
         }
         __syncwarp();
         uint32_t t = 0, un = 0;   // tiles and units of this stream
         bool ok = true, to_release = false;
-        auto release_q = [&]() {   // the output of the last unit has left the place of its queries; the next ones are asked for
+        EncoderBounds ahead = bounds_at(0);
+        auto release_q = [&]() {   // the output of the last unit leaves the place of its queries to the next ones
             if (to_release) {
                 if (lane == 0) {
                     bulk_wait_read<0>();
                     mbar_arrive(q_free0 + 16 * g + 8 * qbuf_of(C::kQBufs == 2 ? un + 1u : 0u));
                 }
-                if (q_loader) load_next_q();
+                if (!C::kLoaderQ && q_loader) load_next_q(ahead);   // (of unit n + 1 = q_next)
                 __syncwarp();
                 to_release = false;
             }
         };
-        EncoderBounds ahead = bounds_at(0);
         for (int32_t n = 0; ok && n < n_units; ++n) {
             const Unit u = unit_at(n);
             const int32_t len = ahead.len(enc), blocks = blocks_of(ahead);
@@ -560,7 +606,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     break;
                 }
                 tc_fence_after();
-                if (!C::kBulkOut && j == n_tiles - 1 && q_loader) load_next_q();   // the last S has landed: its queries are no longer read
+                if (!C::kBulkOut && j == n_tiles - 1 && q_loader) load_next_q(ahead);   // the last S has landed: its queries are no longer read
                 if (warp_live) {
                     const int groups = min(kTileBlocks, blocks - j * kTileBlocks);
                     uint64_t keep = ~0ull;   // a bit per column that holds a key
@@ -709,30 +755,29 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                 const float inv = 1.f / l;
                 const uint32_t place = q_smem + (g * C::kQBufs + qbuf_of(un - 1u)) * C::kQBytes + wq * 32 * 128;
                 uint8_t* mine = smem_raw + (place - raw) + lane * 128;
+                constexpr int kCols = kHeld ? 32 : 64;   // (as many at a time as there are registers for)
 #pragma unroll
-                for (int cb = 0; cb < D / 32; ++cb) {
-                    uint32_t o[32];
-                    tmem_ld32(o_tmem + cb * 32, o);
+                for (int cb = 0; cb < D; cb += kCols) {
+                    uint32_t o[kCols];
+                    if constexpr (kCols == 64) tmem_ld64(o_tmem + cb, o);
+                    else tmem_ld32(o_tmem + cb, o);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 0; c < kCols / 8; ++c) {
                         uint32_t w[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(o[8 * c + 2 * i]) * inv, __uint_as_float(o[8 * c + 2 * i + 1]) * inv);
                             w[i] = *reinterpret_cast<const uint32_t*>(&h);
                         }
-                        *reinterpret_cast<uint4*>(mine + (cb >> 1) * C::kQHalfBytes + ((((cb & 1) * 4 + c) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(mine + (cb >> 6) * C::kQHalfBytes + ((((cb & 63) / 8 + c) ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 }
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    int c[4] = {0, 0, 0, 0};
-                    c[opos.x] = u.qt(g) * kQRows + wq * 32;
-                    c[opos.y] = u.head(g);
-                    c[opos.z] = u.row;
+                    const int3 c = coords(opos, u.qt(g) * kQRows + wq * 32, u.head(g), u.row);
 #pragma unroll
-                    for (int h = 0; h < C::kHalves; ++h) tma_store_4d(&o_map, place + h * C::kQHalfBytes, h * 64, c[1], c[2], c[3]);
+                    for (int h = 0; h < C::kHalves; ++h) tma_store_4d(&o_map, place + h * C::kQHalfBytes, h * 64, c.x, c.y, c.z);
                     bulk_commit();
                 }
             } else if (warp_live && r < valid_rows) {   // a row without keys: zeros
@@ -747,11 +792,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             tc_fence_before();   // the reads of O come before the arrival on p_full for the next unit's first tile
         }
         if (lane == 0) bulk_wait_all();   // the output is written before the CTA ends
-        // query tiles requested but never used must land before that, too
-        if (q_loader)
-            for (uint32_t q = un; q < q_asked; ++q)
-                for (uint32_t i = 0; i < kSpinLimit; ++i)
-                    if (mbar_try_wait(q_full0 + 16 * g + 8 * qbuf_of(q), qpar_of(q))) break;
+        if (!C::kLoaderQ && q_loader && q_asked > 0) await_q(g, q_asked - 1u);
     }
 
     // ---------------------------------------------------------------- teardown
@@ -808,8 +849,11 @@ cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, c
     static SharedMemoryOptIn opt_in;
     const cudaError_t oe = opt_in.ensure(attend_tiles_kernel<D, kHeld>, (int)C::kSmemBytes);
     if (oe != cudaSuccess) return oe;
-    const int64_t grid = std::min<int64_t>(plan.units, (int64_t)sm_count * C::kCtasPerSm);
-    return launch_kernel(true, attend_tiles_kernel<D, kHeld>, dim3((unsigned)grid), dim3(C::kThreads), KernelMemory(C::kSmemBytes), stream, qm,
+    const int64_t slots = (int64_t)sm_count * C::kCtasPerSm, grid = std::min<int64_t>(plan.units, slots), rest = plan.units % slots;
+    // Where SMs hold two CTAs and an eighth to two thirds of them have a unit in the last round, these must not share SMs: launched onto an
+    // idle chip they do not, onto SMs that come free one by one they do (UNEVEN).
+    const bool uneven = C::kCtasPerSm == 2 && plan.units > slots && 8 * rest > slots && 3 * rest <= 2 * slots;
+    return launch_kernel(!uneven, attend_tiles_kernel<D, kHeld>, dim3((unsigned)grid), dim3(C::kThreads), KernelMemory(C::kSmemBytes), stream, qm,
                          make_int3(pos[0], pos[1], pos[2]), om, make_int3(opos[0], opos[1], opos[2]), km, vm, vm16, make_int3(kpos[0], kpos[1], kpos[2]),
                          (__nv_bfloat16*)O.ptr, O.row, O.head, O.token, enc, held, T, plan,
                          softmax_scale * 1.4426950408889634f, status);
