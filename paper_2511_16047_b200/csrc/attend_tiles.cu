@@ -155,7 +155,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
         }
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(smem_u32(&bars->kv_full[s]), kHeld ? C::kLoadWarps : 33);   // (the lanes of the one loading warp, and its bulk copies)
-            mbar_init(smem_u32(&bars->kv_empty[s]), C::kMmaWarps);   // one arrival per issuing warp, or two of the one whose tile it is
+            mbar_init(smem_u32(&bars->kv_empty[s]), C::kMmaWarps);   // one arrival per issuing warp, whether it uses the tile or passes it
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -464,7 +464,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
         // of each stream: the tile whose P V is due; tiles and units begun
         uint32_t pv_stage[kStreams] = {}, pv_nch[kStreams] = {}, pv_first[kStreams] = {}, t[kStreams] = {}, un[kStreams] = {};
         uint32_t stage = 0, phase = 0;   // of the next tile
-        bool shared = false, alone = false;   // the unit's tiles are for both streams; for this warp's alone
+        bool shared = false;             // the unit's tiles are for both streams
         auto issue_pv = [&](const int i, const uint32_t last) -> bool {
             const int g = kStreams == 2 ? i : my_g;
             const uint32_t tile = t[i] - 1u, buf = buf_of(tile);
@@ -475,10 +475,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             // (one issuer and shared tiles: the second stream's product, behind the first's, frees the stage)
             umma_pv(tmem + C::kOCol + g * D, tmem + C::kSCol + (g * C::kSBufs + buf) * kKT, v_lo0 + pv_stage[i] * kStageLo, kDescHi, idesc_pv,
                     pv_first[i] ^ 1u, pv_nch[i], kStreams == 2 && i == 0 ? (shared ? 0u : 1u) : 1u, empty, last, o_full0 + 8 * g);
-            if (C::kMmaWarps == 2) {
-                if (alone) umma_commit_elected(empty);
-                umma_commit_elected(pv_done0 + 8 * g);
-            }
+            if (C::kMmaWarps == 2) umma_commit_elected(pv_done0 + 8 * g);
             return true;
         };
         auto step = [&]() {
@@ -486,6 +483,16 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                 stage = 0;
                 phase ^= 1u;
             }
+        };
+        // Two issuing warps: a tile of the other's stream is waited for and given back all the same.  A wait tells one phase of a stage from the
+        // one before it only, so that a warp which left tiles out could take the landing of an older tile for that of its own, or,
+        // while the other frees and fills the stage without it, fall two phases behind.
+        auto pass = [&]() -> bool {
+            if (!await(kv_full0 + 8 * stage, phase)) return false;
+            if (lane == 0) mbar_arrive(kv_empty0 + 8 * stage);
+            __syncwarp();
+            step();
+            return true;
         };
         EncoderBounds ahead = bounds_at(0);
         for (int32_t n = 0; n < n_units; ++n) {
@@ -495,9 +502,9 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             const int n_tiles = (blocks + kTileBlocks - 1) / kTileBlocks;
             const bool apart = u.two && !u.shared;
             shared = u.shared;
-            alone = !u.shared;
             if (kStreams == 1 && my_g == 1 && !u.two) {
-                for (int j = 0; j < n_tiles; ++j) step();
+                for (int j = 0; j < n_tiles; ++j)
+                    if (!pass()) goto stopped;
                 continue;
             }
             for (int j = 0; j < n_tiles; ++j) {
@@ -509,7 +516,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                 for (int i = 0; i < kStreams; ++i) {
                     const int g = kStreams == 2 ? i : my_g;
                     if (kStreams == 2 && i == 1 && !u.two) continue;
-                    if (kStreams == 1 && apart && g == 1) step();   // (stream A's tile)
+                    if (kStreams == 1 && apart && g == 1 && !pass()) goto stopped;   // (stream A's tile)
                     const uint32_t qb = qbuf_of(un[i] - (j == 0 ? 0u : 1u));
                     if (j == 0) {
                         if (!await(q_full0 + 16 * g + 8 * qb, qpar_of(un[i]))) goto stopped;
@@ -532,7 +539,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     if (kStreams == 2 && apart && i == 0) step();
                 }
                 step();
-                if (kStreams == 1 && apart && my_g == 0) step();    // (stream B's tile)
+                if (kStreams == 1 && apart && my_g == 0 && !pass()) goto stopped;    // (stream B's tile)
             }
             // The last P V of the unit does not wait for the next unit's first S: its output is due.
 #pragma unroll

@@ -55,6 +55,11 @@ SHAPES = [
     (9, 3, 3, 64, 18, 333),        # 324 queries: three tiles
     (3, 3, 3, 128, 20, 65),
     (2, 2, 2, 128, 32, 1100),
+    # several units per CTA: streams with tiles of their own, and (an odd number of them) one alone in a unit
+    (40, 16, 16, 128, 2, 150),
+    (110, 3, 3, 128, 2, 130),
+    (130, 5, 5, 64, 2, 100),
+    (50, 3, 1, 128, 16, 70),
 ]
 
 

@@ -62,6 +62,8 @@ def _check(out, q, ks, vs, kept, scale, what):
     (3, 1, 128, (4, 8, 12, 13, 18), (0, 1, True)),
     (1, 2, 64, (9, 2, 14, 1, 3), (1, 1, False)),       # scales that shrink: few queries, many keys
     (1, 2, 128, (20, 1, 4), (0, 1, True)),
+    (110, 3, 128, (2, 7, 3), (0, 1, True)),            # several units per CTA, a stream alone in every other one
+    (80, 9, 64, (3, 5), (0, 1, True)),
 ])
 def test_a_schedule(rows, heads, D, sides, policy, path):
     steps = _steps(rows, heads, sides, D, sum(sides) + D)
