@@ -267,13 +267,25 @@ void note_appended(amskv_cache* cache, int layer, int scale)
     cache->last_appended[layer] = scale;
 }
 
-// whether the tensor-memory kernel serves a call over an encoder's states or a cache held in 8 bits, else the warp-matrix kernel
-bool takes_tiles(const amskv_cache* cache, int32_t T, int32_t group, int32_t kv_heads, int64_t keys)
+// Whether the tensor-memory kernel (attend_tiles.cu) serves a call over an encoder's states or a cache held in 8 bits, else the
+// warp-matrix kernel (attend_rows.cu), which wins where its CTAs of up to 64 query rows all run at once, sharing long keys
+// between them, and where 16 rows or fewer leave the other's tiles of 128 empty.  `items`: rows x key/value heads; `group` query heads share one.
+// us per call, warp-matrix / tensor-memory, in a graph, 256 keys where nothing else is said:
+//   64 channels, an encoder:   T = 16  512 items 6.6 / 10.2, 8 192 88 / 99 (77 keys 67 / 60);  T = 36  128 6.3 / 8.9, 512 11.8 / 10.6;
+//     T = 100  128 (two CTAs each) 8.4 / 9.5, 512 24.5 / 12.4;  T = 144  32 8.9 / 12.3, 128 (three) 13.0 / 10.2;  T = 576  32 10.1 / 10.8
+//   64 channels, 8 bits:       T = 36  512 14.2 / 16.1, 2 048 53 / 56;  T = 64  2 048 60 / 62, 8 192 219 / 204;  T = 100  128 10.3 / 14.9, 512 29.8 / 17.2
+//   128 channels, an encoder:  T = 16  512 12.2 / 16.5, 8 192 184 / 205 (77 keys 127 / 111);  T = 64  128 9.3 / 9.6 (512 keys 15.0 / 13.5, 1 024 21.5 / 23.5),
+//     512 26.2 / 17.5;  T = 100  32 10.3 / 10.9, 128 (two CTAs each) 11.9 / 10.0;  T = 144  32 13.2 / 12.9
+//   128 channels, 8 bits:      T = 36  128 12.3 / 12.6, 512 30.4 / 23.8;  T = 100  32 11.2 / 12.8, 128 15.7 / 13.1;  T = 144  32 13.4 / 11.9
+bool takes_tiles(const amskv_cache* cache, int32_t T, int32_t group, int64_t items, int64_t keys)
 {
-    (void)group, (void)kv_heads, (void)keys;
     if (!cache->tc_ready || cache->path == AMSKV_PATH_SMALL || cache->path == AMSKV_PATH_SIMT) return false;
     if (cache->path != AMSKV_PATH_AUTO) return true;
-    return T > 64;
+    const int64_t M = (int64_t)T * group, sms = cache->sm_count, ctas = items * ((M + 63) / 64);
+    if (M <= 16) return items > 16 * sms && keys <= 256;
+    if (M <= 32 && items <= 4 * sms) return false;
+    if (cache->head_dim == 64) return ctas > 2 * sms && !(cache->held() && M <= 64 && items <= 16 * sms);
+    return M > 128 || ctas > sms;
 }
 
 // which kernel amskv_attend uses for T query tokens over `total` keys
@@ -490,7 +502,7 @@ int amskv_attend(amskv_cache* cache, int layer, int scale, const void* Q, void* 
         HeldKeys keys{region.codes, region.scales, region.capacity, 0, ranges};
         for (int i = 0; i < ranges.n; ++i) keys.blocks += (ranges.r[i].len + kBlock - 1) / kBlock;
         e = cudaErrorNotSupported;
-        if (takes_tiles(cache, T, 1, cache->heads, (int64_t)keys.blocks * kBlock))
+        if (takes_tiles(cache, T, 1, cache->items(), (int64_t)keys.blocks * kBlock))
             e = launch_attend_tiles(q, o, keys, T, cache->rows, cache->heads, cache->head_dim, cache->softmax_scale, cache->status_word(),
                                     cache->sm_count, static_cast<cudaStream_t>(stream));
         if (e == cudaErrorNotSupported)   // (strides that no tensor map holds, too)
@@ -826,7 +838,7 @@ int amskv_cross_attend(amskv_cache* cache, int scale, const amskv_encoder* enc, 
                            kv_rows == cache->rows && k.row != 0 && !enc->offsets};
     const int32_t group = cache->heads / enc->kv_heads;
     cudaError_t e = cudaErrorNotSupported;
-    if (takes_tiles(cache, T, group, enc->kv_heads, keys.max_keys))
+    if (takes_tiles(cache, T, group, (int64_t)cache->rows * enc->kv_heads, keys.max_keys))
         e = launch_attend_tiles(q, o, keys, T, cache->rows, enc->kv_heads, group, cache->head_dim, cache->softmax_scale, cache->status_word(),
                                 cache->sm_count, static_cast<cudaStream_t>(stream));
     if (e == cudaErrorNotSupported)   // (strides that no tensor map holds, too)

@@ -33,7 +33,7 @@ struct RowsCfg {
     static constexpr int kPartBytes = 16 * kPartRow * 4;                    // products of a warp's 16 rows
     static constexpr int kStatsAt = kWarps * kPartBytes;                    // maxima and sums of the rows behind them
     static constexpr int kSmemBytes = kStages * kStageBytes;
-    static_assert(kStatsAt + kWarps * 16 * 8 <= kSmemBytes, "the parts take the place of the stages");
+    static_assert(kStatsAt + 2 * kWarps * 16 * 8 <= kSmemBytes, "the parts take the place of the stages");
 };
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -301,46 +301,100 @@ attend_rows_kernel(const __nv_bfloat16* Q, int64_t q_row, int64_t q_head, int64_
         stats[g] = make_float2(m_a, l_a);
         stats[g + 8] = make_float2(m_b, l_b);
     }
-    if (splits > 1) ptx::cluster_sync();
-    else __syncthreads();
-    // each CTA of the cluster finishes its share of the channels, eight at a time
-    const int32_t pieces = D / 8 / splits;
-    for (int32_t i = threadIdx.x; i < kQB * 16 * pieces; i += kThreads) {
-        const int32_t r = i / pieces, piece = rank * pieces + i - r * pieces;   // row among the CTA's kQB x 16
-        const int32_t m = part * kQB * 16 + r;
-        if (m >= M) continue;
+    __syncthreads();
+    // the parts of this CTA's warps, eight channels of a row at a time, into the place of the first (or out)
+    const float2* all_stats = reinterpret_cast<const float2*>(smem + C::kStatsAt);
+    constexpr int32_t kPieceRounds = kQB * 16 * (D / 8) / kThreads;
+#pragma unroll
+    for (int32_t i = 0; i < kPieceRounds; ++i) {
+        if (kKS == 1 && splits > 1) break;   // (a row has one part already)
+        const int32_t at = i * kThreads + threadIdx.x, r = at / (D / 8), c = at % (D / 8) * 8, w0 = r / 16 * kKS;   // row among the CTA's kQB x 16
+        float2 ml[kKS];
         float top = -INFINITY;
-        for (int32_t n = 0; n < splits * kKS; ++n) {
-            const uint32_t at = smem0 + C::kStatsAt + (((r / 16) * kKS + n % kKS) * 16 + r % 16) * 8;
-            top = fmaxf(top, ld_cluster_8B(ptx::map_to_rank(at, n / kKS)).x);
+#pragma unroll
+        for (int n = 0; n < kKS; ++n) {
+            ml[n] = all_stats[(w0 + n) * 16 + r % 16];
+            top = fmaxf(top, ml[n].x);
         }
         float l = 0.f, acc[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-        if (top != -INFINITY) {   // (a row without a key: zeros)
-            for (int32_t n = 0; n < splits * kKS; ++n) {
-                const uint32_t w = (uint32_t)((r / 16) * kKS + n % kKS);
-                const float2 ml = ld_cluster_8B(ptx::map_to_rank(smem0 + C::kStatsAt + (w * 16 + r % 16) * 8, n / kKS));
-                const float f = fast_exp2((ml.x - top) * scale_log2);
-                const uint32_t at = ptx::map_to_rank(smem0 + w * C::kPartBytes + ((r % 16) * C::kPartRow + piece * 8) * 4, n / kKS);
-                const float4 a = ld_cluster_16B(at), b = ld_cluster_16B(at + 16);
-                l = fmaf(ml.y, f, l);
-                acc[0] = fmaf(a.x, f, acc[0]);
-                acc[1] = fmaf(a.y, f, acc[1]);
-                acc[2] = fmaf(a.z, f, acc[2]);
-                acc[3] = fmaf(a.w, f, acc[3]);
-                acc[4] = fmaf(b.x, f, acc[4]);
-                acc[5] = fmaf(b.y, f, acc[5]);
-                acc[6] = fmaf(b.z, f, acc[6]);
-                acc[7] = fmaf(b.w, f, acc[7]);
-            }
+        float* first = reinterpret_cast<float*>(smem + w0 * C::kPartBytes) + r % 16 * C::kPartRow + c;
+#pragma unroll
+        for (int n = 0; n < kKS; ++n) {
+            const float f = top == -INFINITY ? 0.f : fast_exp2((ml[n].x - top) * scale_log2);   // (a row without a key: zeros)
+            l = fmaf(ml[n].y, f, l);
+            const float4 x = *reinterpret_cast<const float4*>(first + n * (C::kPartBytes / 4)), y = *reinterpret_cast<const float4*>(first + n * (C::kPartBytes / 4) + 4);
+            acc[0] = fmaf(x.x, f, acc[0]);
+            acc[1] = fmaf(x.y, f, acc[1]);
+            acc[2] = fmaf(x.z, f, acc[2]);
+            acc[3] = fmaf(x.w, f, acc[3]);
+            acc[4] = fmaf(y.x, f, acc[4]);
+            acc[5] = fmaf(y.y, f, acc[5]);
+            acc[6] = fmaf(y.z, f, acc[6]);
+            acc[7] = fmaf(y.w, f, acc[7]);
         }
-        const float inv = top != -INFINITY ? 1.f / l : 0.f;
-        *reinterpret_cast<uint4*>(O + row * o_row + row_offset(m, o_head, o_tok) + piece * 8) =
-            make_uint4(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv),
-                       pack_bf16(acc[4] * inv, acc[5] * inv), pack_bf16(acc[6] * inv, acc[7] * inv));
+        if (splits == 1) {
+            const int32_t m = part * kQB * 16 + r;
+            if (m < M) {
+                const float inv = l > 0.f ? 1.f / l : 0.f;
+                *reinterpret_cast<uint4*>(O + row * o_row + row_offset(m, o_head, o_tok) + c) =
+                    make_uint4(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv),
+                               pack_bf16(acc[4] * inv, acc[5] * inv), pack_bf16(acc[6] * inv, acc[7] * inv));
+            }
+        } else {
+            *reinterpret_cast<float4*>(first) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            *reinterpret_cast<float4*>(first + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+            // the row's maximum and sum, beside the parts' (which other threads may still read)
+            if (c == 0) reinterpret_cast<float2*>(smem + C::kStatsAt)[kWarps * 16 + r] = make_float2(top, l);
+        }
     }
-    if (splits > 1) ptx::cluster_sync();   // nobody's parts go while another reads them
+    if (splits == 1) return;
+    // the parts of the cluster's CTAs: each finishes its share of the channels, kWide at a time, and asks for all parts before it uses one
+    ptx::cluster_sync();
+    constexpr int kMaxSplits = 8, kWide = kQB == 4 ? 8 : 4;
+    const uint32_t stats_at = smem0 + C::kStatsAt + (kKS == 1 ? 0 : kWarps * 16 * 8);
+    const int32_t pieces = D / kWide / splits;
+    for (int32_t i = threadIdx.x; i < kQB * 16 * pieces; i += kThreads) {
+        const int32_t r = i / pieces, c = (rank * pieces + i - r * pieces) * kWide, m = part * kQB * 16 + r;
+        if (m >= M) continue;
+        float2 ml[kMaxSplits];
+        float4 x[kMaxSplits][kWide / 4];
+        float top = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < kMaxSplits; ++n)
+            if (n < splits) {
+                ml[n] = ld_cluster_8B(ptx::map_to_rank(stats_at + r * 8, n));
+                const uint32_t from = ptx::map_to_rank(smem0 + r / 16 * kKS * C::kPartBytes + (r % 16 * C::kPartRow + c) * 4, n);
+#pragma unroll
+                for (int e = 0; e < kWide / 4; ++e) x[n][e] = ld_cluster_16B(from + 16 * e);
+            }
+#pragma unroll
+        for (int n = 0; n < kMaxSplits; ++n)
+            if (n < splits) top = fmaxf(top, ml[n].x);
+        float l = 0.f, acc[kWide];
+#pragma unroll
+        for (int e = 0; e < kWide; ++e) acc[e] = 0.f;
+#pragma unroll
+        for (int n = 0; n < kMaxSplits; ++n)
+            if (n < splits) {
+                const float f = top == -INFINITY ? 0.f : fast_exp2((ml[n].x - top) * scale_log2);
+                l = fmaf(ml[n].y, f, l);
+#pragma unroll
+                for (int e = 0; e < kWide / 4; ++e) {
+                    acc[4 * e] = fmaf(x[n][e].x, f, acc[4 * e]);
+                    acc[4 * e + 1] = fmaf(x[n][e].y, f, acc[4 * e + 1]);
+                    acc[4 * e + 2] = fmaf(x[n][e].z, f, acc[4 * e + 2]);
+                    acc[4 * e + 3] = fmaf(x[n][e].w, f, acc[4 * e + 3]);
+                }
+            }
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        uint2* dst = reinterpret_cast<uint2*>(O + row * o_row + row_offset(m, o_head, o_tok) + c);
+#pragma unroll
+        for (int e = 0; e < kWide / 4; ++e)
+            dst[e] = make_uint2(pack_bf16(acc[4 * e] * inv, acc[4 * e + 1] * inv), pack_bf16(acc[4 * e + 2] * inv, acc[4 * e + 3] * inv));
+    }
+    ptx::cluster_sync();   // nobody's parts go while another reads them
 }
 
 template <int D, int kQB, bool kHeld>
@@ -353,9 +407,12 @@ cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, c
     if (oe != cudaSuccess) return oe;
     const int64_t blocks = ((int64_t)T * group + 15) / 16, parts = (blocks + kQB - 1) / kQB, ctas = parts * rows * kv_heads;
     // Few CTAs and several chunks of keys: clusters share them.
+    // A merge of 64 rows costs what several chunks do, of codes fewer (128 channels, 32 items, 256 keys, shared from 4 chunks a CTA / from 8:
+    // T = 16 6.7 / -, T = 36 9.8 / 9.7, T = 144 14.6 / 13.2; 8 bits, T = 36 9.7 / 12.0 us; two chunks are not shared: T = 16, 77 keys 4.4 / 6.3).
+    constexpr int kMinChunks = kQB == 4 && !kHeld ? 8 : 4;
     const int64_t chunks = (max_keys + kChunk - 1) / kChunk;
     int32_t splits = 1;
-    while (splits < 8 && ctas * splits * 2 <= 2ll * sm_count && chunks >= splits * 2) splits *= 2;
+    while (splits < 8 && ctas * splits * 2 <= 2ll * sm_count && chunks >= splits * kMinChunks) splits *= 2;
     if (ctas * splits > 0x7fffffffll) return cudaErrorInvalidValue;
     return launch_kernel(true, attend_rows_kernel<D, kQB, kHeld>, dim3((unsigned)(ctas * splits)), dim3(kThreads),
                          KernelMemory(C::kSmemBytes, (unsigned)splits), stream, (const __nv_bfloat16*)Q.ptr, Q.row, Q.head, Q.token,
