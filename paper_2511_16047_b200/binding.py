@@ -142,7 +142,8 @@ def _check(code: int, where: str) -> None:
 # The calls of a generation step go through the _steps module where it is built, which takes addresses and strides out of the
 # tensors natively; it returns None for arguments of other than the usual forms, and the call is made through ctypes.
 if _steps is not None:
-    _steps.bind(*(ctypes.cast(fn, ctypes.c_void_p).value for fn in (lib.amskv_append, lib.amskv_attend, lib.amskv_append_attend)))
+    _steps.bind(*(ctypes.cast(fn, ctypes.c_void_p).value for fn in (lib.amskv_append, lib.amskv_attend, lib.amskv_append_attend, lib.amskv_rotary,
+                                                                            lib.amskv_cross_attend)))
 
 
 def _int32(name: str, x) -> None:
@@ -287,8 +288,13 @@ def amskv_cross_attend(cache: int, scale: int, kv_heads: int, keys: int, K, V, Q
                        stream=None) -> None:
     """The queries of `scale` over an encoder's states: K and V [rows, kv_heads, keys, D] with device int32 `lengths` [rows], or,
     with device int32 `offsets` [rows + 1], [1, kv_heads, keys, D] (all rows one behind the other)."""
+    if _steps is not None:
+        rc = _steps.cross_attend(cache, scale, kv_heads, keys, K, V, Q, out, lengths, offsets, max_keys, stream)
+        if rc is not None:
+            return _check(rc, "amskv_cross_attend")
     for name, x in (("scale", scale), ("kv_heads", kv_heads), ("keys", keys), ("max_keys", max_keys)):
         _int32(name, x)
+    assert all(not hasattr(x, "is_contiguous") or x.is_contiguous() for x in (lengths, offsets)), "expected contiguous lists"
     enc = Encoder(kv_heads, keys, max_keys, _addr(lengths), _addr(offsets))
     _check(lib.amskv_cross_attend(cache, scale, ctypes.byref(enc), _addr(K), _addr(V), _kv_strides(K, V), _addr(Q), _addr(out), _strides(Q),
                                   _strides(out), _stream(stream)), "amskv_cross_attend")
@@ -354,6 +360,11 @@ def amskv_rotary(spec: RotarySpec, table, table_rows: int, first: int, index, ro
                  Q_out, k_heads: int = 0, K=None, K_out=None, transposed: bool = False, stream=None, index_row_stride=None) -> None:
     """Rotates Q (and K) by rows first .. first + T - 1 of the table, or by the rows `index` names: device int32 [T] or
     [rows, T] (a tensor, or an address with index_row_stride)."""
+    if _steps is not None:
+        rc = _steps.rotary(spec, table, table_rows, first, index, index_row_stride, rows, T, head_dim, q_heads, Q, Q_out, k_heads, K, K_out,
+                           transposed, stream)
+        if rc is not None:
+            return _check(rc, "amskv_rotary")
     if index_row_stride is None:
         index_row_stride = 0
         if hasattr(index, "stride"):

@@ -12,6 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libamskv.so")
 STEPS = os.path.join(HERE, "_steps" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 STEPS_SOURCE = os.path.join(CSRC, "steps.c")
+STEPS_DEPS = [STEPS_SOURCE, os.path.join(HERE, "..", "include", "amskv.h")]
 SOURCES = ["api.cu", "append.cu", "attend_simt.cu", "attend_tc.cu", "attend_pair.cu", "attend_small.cu", "attend_mid.cu", "similarity.cu", "density.cu", "rotary.cu", "held.cu", "attend_rows.cu", "attend_tiles.cu", "selftest.cu"]
 HEADERS = ["kernels.cuh", "keys.cuh", "policy.hpp", "sm100_ptx.cuh", os.path.join("..", "..", "include", "amskv.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -35,7 +36,7 @@ def _stale() -> bool:
 
 def build_steps(force: bool = False) -> str:
     """Compile the binding's CPython module for the running interpreter."""
-    if not force and os.path.exists(STEPS) and os.path.getmtime(STEPS) >= os.path.getmtime(STEPS_SOURCE):
+    if not force and os.path.exists(STEPS) and all(os.path.getmtime(STEPS) >= os.path.getmtime(d) for d in STEPS_DEPS):
         return STEPS
     tmp = STEPS + ".tmp.%d" % os.getpid()
     try:

@@ -251,7 +251,7 @@ RotaryFrequencies rotary_frequencies(const amskv_rotary_spec& s)
             const double g = std::min(std::max((i - lo) / (hi - lo), 0.0), 1.0);
             w = w * (1.0 - g) + w / s.factor * g;
         }
-        f.half_turns[i] = w / kPi;
+        f.turns[i] = (uint64_t)std::ldexp(w / (2.0 * kPi), 64);   // (w <= 1)
     }
     return f;
 }

@@ -153,10 +153,10 @@ cudaError_t launch_zero(double* p, size_t n, cudaStream_t stream);
 cudaError_t launch_density(const Strided& Q, const LayerRegion& region, const DensityPieces& pieces, int32_t T,
                            int32_t rows, int32_t heads, int32_t D, float softmax_scale, double* out, cudaStream_t stream);
 
-// Rotary positions (rotary.cu).  Frequencies of one axis, in half turns per unit of position; every axis has the same.
+// Rotary positions (rotary.cu).  Frequencies of one axis, in 2^-64 turns per unit of position; every axis has the same.
 constexpr int kMaxRotaryDim = 256;
 struct RotaryFrequencies {
-    double half_turns[kMaxRotaryDim / 2];
+    uint64_t turns[kMaxRotaryDim / 2];
     int32_t n, axes;
     float amplitude;
 };

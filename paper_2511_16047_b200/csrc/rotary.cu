@@ -12,20 +12,46 @@ namespace {
 constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------- the table
-// Entry (n, column) = (cos, sin) of positions[n][axis] * frequency, times the amplitude.  The angle is formed and reduced in 64 bits,
-// in half turns (the host divides the frequencies by pi): at position 10^6 an fp32 angle would be off by 0.06.  What is left,
-// within a quarter turn either way, is rounded to fp32 once (an angle error of 2^-26 pi) and goes through sincospif.
-// Four rows of a thread at a time: with one, the loop waits for its position.  131 071 x 64: 27.4 -> TABLE us.
-constexpr int kTableRows = 4;
+// Entry (n, column) = (cos, sin) of positions[n][axis] * frequency, times the amplitude.  An fp32 angle would be off by 0.06 at position
+// 10^6.  The frequency is a fraction of a turn in 64 bits, the position 24 bits and an exponent: their product, shifted, loses whole turns by
+// wrapping around, which is all the range reduction there is, without a double-precision instruction (their rounding and
+// conversions run at a sixteenth of the rate: 131 071 x 64 27.4 us with them).  What is left, within a quarter turn of a whole or half
+// one, is rounded to fp32 once and goes through sincospif.
+__device__ __forceinline__ float2 table_entry(float position, uint64_t turns, float amplitude)
+{
+    const uint32_t bits = __float_as_uint(position), exponent = (bits >> 23) & 0xffu;
+    const uint32_t m = exponent ? (bits & 0x7fffffu) | 0x800000u : bits & 0x7fffffu;
+    const int32_t shift = (exponent ? (int32_t)exponent : 1) - 150;   // position = +-m * 2^shift
+    // m * turns, 88 bits
+    const uint64_t p0 = (uint64_t)m * (uint32_t)turns, p1 = (uint64_t)m * (uint32_t)(turns >> 32), lo = p0 + (p1 << 32);
+    const uint64_t hi = (p1 >> 32) + (lo < p0 ? 1u : 0u);
+    uint64_t phase;   // in 2^-64 turns, whole turns gone
+    if (shift >= 0) phase = shift < 64 ? lo << shift : 0;
+    else if (shift > -64) phase = (lo >> -shift) | (hi << (64 + shift));
+    else phase = shift > -128 ? hi >> (-64 - shift) : 0;
+    const uint32_t x = (uint32_t)((bits >> 31 ? 0ull - phase : phase) >> 32);
+    const uint32_t half = (x + 0x40000000u) >> 31;                    // nearer to half a turn than to a whole one
+    float s, c;
+    sincospif((float)(int32_t)(x ^ (half << 31)) * 4.656612873077393e-10f /* 2^-31 */, &s, &c);
+    float a = half ? -amplitude : amplitude;
+    if (exponent == 255) a = __uint_as_float(0x7fc00000u);            // (no position has no angle)
+    return make_float2(c * a, s * a);
+}
+
+constexpr int kTableRows = 4;   // rows of a thread on their way at a time
+// kCols neighbouring columns a thread (two where an axis has an even number of them: 16-byte stores).
+template <int kCols>
 __global__ void __launch_bounds__(kThreads)
 rotary_table_kernel(const float* positions, const __grid_constant__ RotaryFrequencies freq, int64_t count, float2* table)
 {
-    const int32_t cols = freq.axes * freq.n, per_pass = kThreads / cols;
-    const int32_t row0 = (int32_t)threadIdx.x / cols, col = (int32_t)threadIdx.x - row0 * cols;
+    const int32_t cols = freq.axes * freq.n, groups = cols / kCols, per_pass = kThreads / groups;
+    const int32_t row0 = (int32_t)threadIdx.x / groups, col = ((int32_t)threadIdx.x - row0 * groups) * kCols;
     overlap_with_previous();
     if (row0 >= per_pass) return;
     const int32_t axis = col / freq.n;
-    const double half_turns = freq.half_turns[col - axis * freq.n];
+    uint64_t turns[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) turns[c] = freq.turns[col - axis * freq.n + c];
     const int64_t step = (int64_t)gridDim.x * per_pass;
     for (int64_t row = (int64_t)blockIdx.x * per_pass + row0; row < count; row += kTableRows * step) {
         float pos[kTableRows];
@@ -34,12 +60,12 @@ rotary_table_kernel(const float* positions, const __grid_constant__ RotaryFreque
 #pragma unroll
         for (int i = 0; i < kTableRows; ++i) {
             if (row + i * step >= count) break;
-            const double t = (double)pos[i] * half_turns;
-            const double f = fma(-2.0, rint(0.5 * t), t), n = rint(f);   // f in [-1, 1]
-            float s, c;
-            sincospif((float)(f - n), &s, &c);
-            const float a = n != 0.0 ? -freq.amplitude : freq.amplitude;
-            table[(row + i * step) * cols + col] = make_float2(c * a, s * a);
+            float2 e[kCols];
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) e[c] = table_entry(pos[i], turns[c], freq.amplitude);
+            float2* dst = table + (row + i * step) * cols + col;
+            if constexpr (kCols == 2) *reinterpret_cast<float4*>(dst) = make_float4(e[0].x, e[0].y, e[1].x, e[1].y);
+            else dst[0] = e[0];
         }
     }
 }
@@ -208,10 +234,10 @@ rotary_any_kernel(const __grid_constant__ RotaryArgs a)
 cudaError_t launch_rotary_table(const float* positions, const RotaryFrequencies& freq, int64_t count, float2* table, int sm_count,
                                 cudaStream_t stream)
 {
-    const int32_t per_pass = kThreads / (freq.axes * freq.n);
+    const int32_t wide = freq.n % 2 == 0 ? 2 : 1, per_pass = kThreads / (freq.axes * freq.n / wide);
     const int64_t blocks = std::min<int64_t>((count + per_pass - 1) / per_pass, 8ll * sm_count);
-    return launch_kernel(true, rotary_table_kernel, dim3((unsigned)blocks), dim3(kThreads), KernelMemory(0), stream, positions, freq,
-                         count, table);
+    return launch_kernel(true, wide == 2 ? rotary_table_kernel<2> : rotary_table_kernel<1>, dim3((unsigned)blocks), dim3(kThreads), KernelMemory(0),
+                         stream, positions, freq, count, table);
 }
 
 cudaError_t launch_rotary(const RotaryArgs& a, int sm_count, cudaStream_t stream)

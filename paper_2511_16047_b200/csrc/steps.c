@@ -1,4 +1,4 @@
-/* Python side of the calls of a generation step (amskv_append, amskv_attend, amskv_append_attend): takes addresses and strides
+/* Python side of the calls of a generation step (amskv_append, amskv_attend, amskv_append_attend, amskv_rotary, amskv_cross_attend): takes addresses and strides
  * out of the tensors and calls the library, without the argument conversions of ctypes.  Marshalling only, and only of the
  * usual forms: a call with any other argument returns None without having called the library, and the binding makes it
  * through ctypes, which decides what is accepted and what the error is.
@@ -14,6 +14,14 @@
 #include <Python.h>
 #include <stdint.h>
 
+#include "../../include/amskv.h"
+
+typedef int (*rotary_fn)(const amskv_rotary_spec*, const float*, int64_t, int64_t, const int32_t*, int64_t, int, int, int, int, const void*,
+                         const int64_t*, void*, const int64_t*, int, const void*, const int64_t*, void*, const int64_t*, uint32_t, void*);
+typedef int (*cross_fn)(void*, int, const amskv_encoder*, const void*, const void*, const int64_t*, const void*, void*, const int64_t*,
+                        const int64_t*, void*);
+static rotary_fn f_rotary;
+static cross_fn f_cross;
 typedef int (*append_fn)(void*, int, int, const void*, const void*, const int64_t*, void*);
 typedef int (*attend_fn)(void*, int, int, const void*, void*, const int64_t*, const int64_t*, void*);
 typedef int (*append_attend_fn)(void*, int, int, const void*, const void*, const int64_t*, const void*, void*, const int64_t*,
@@ -61,6 +69,42 @@ static int tensor(PyObject* x, void** addr, int64_t* strides, int* strided)
     }
     Py_DECREF(r);
     *strided = 1;
+    return ok ? 0 : -1;
+}
+
+static int as_int(PyObject* o, int* out)
+{
+    if (!PyLong_CheckExact(o)) return -1;
+    const long v = PyLong_AsLong(o);
+    *out = (int)v;
+    return PyErr_Occurred() || v != *out ? -1 : 0;
+}
+
+static int as_int64(PyObject* o, int64_t* out)
+{
+    if (!PyLong_CheckExact(o)) return -1;
+    *out = PyLong_AsLongLong(o);
+    return PyErr_Occurred() ? -1 : 0;
+}
+
+/* address of a list of table rows, and the stride of its rows: None, an int with `given`, or a tensor [T] or [rows, T] */
+static int index_of(PyObject* x, PyObject* given, void** addr, int64_t* row_stride)
+{
+    *row_stride = 0;
+    if (given != Py_None && as_int64(given, row_stride)) return -1;
+    if (x == Py_None || PyLong_CheckExact(x)) return as_pointer(x, addr);
+    PyObject* r = PyObject_CallMethodNoArgs(x, s_data_ptr);
+    if (!r) return -1;
+    const int bad = as_pointer(r, addr);
+    Py_DECREF(r);
+    if (bad) return -1;
+    r = PyObject_CallMethodNoArgs(x, s_stride);
+    if (!r) return -1;
+    const Py_ssize_t n = PyTuple_Check(r) ? PyTuple_GET_SIZE(r) : 0;
+    int64_t last = 0, first = 0;
+    int ok = (n == 1 || n == 2) && !as_int64(PyTuple_GET_ITEM(r, n - 1), &last) && last == 1 && !as_int64(PyTuple_GET_ITEM(r, 0), &first);
+    Py_DECREF(r);
+    if (given == Py_None) *row_stride = n == 2 ? first : 0;
     return ok ? 0 : -1;
 }
 
@@ -151,15 +195,71 @@ static PyObject* py_append_attend(PyObject* self, PyObject* const* args, Py_ssiz
     return PyLong_FromLong(rc);
 }
 
-/* bind(append, attend, append_attend): addresses of the library's functions */
+/* rotary(spec, table, table_rows, first, index, index_row_stride, rows, T, head_dim, q_heads, Q, Q_out, k_heads, K, K_out, transposed, stream) */
+static PyObject* py_rotary(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    void *table, *index, *q, *qo, *k, *ko, *stream;
+    int64_t table_rows, first, index_row, qs[3], qos[3], ks[3], kos[3];
+    int rows, T, d, qh, kh, qv, qov, kv, kov, rc;
+    Py_buffer spec;
+    if (count(n, 17)) return NULL;
+    if (!PyObject_CheckBuffer(a[0]) || PyObject_GetBuffer(a[0], &spec, PyBUF_SIMPLE)) return left_to_ctypes();
+    if (spec.len != (Py_ssize_t)sizeof(amskv_rotary_spec) || tensor(a[1], &table, qs, &qv) || qv || as_int64(a[2], &table_rows) ||
+        as_int64(a[3], &first) || index_of(a[4], a[5], &index, &index_row) || as_int(a[6], &rows) || as_int(a[7], &T) || as_int(a[8], &d) ||
+        as_int(a[9], &qh) || tensor(a[10], &q, qs, &qv) || tensor(a[11], &qo, qos, &qov) || as_int(a[12], &kh) || tensor(a[13], &k, ks, &kv) ||
+        tensor(a[14], &ko, kos, &kov) || (a[15] != Py_True && a[15] != Py_False) || stream_of(a[16], &stream)) {
+        PyBuffer_Release(&spec);
+        return left_to_ctypes();
+    }
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_rotary(spec.buf, table, table_rows, first, index, index_row, rows, T, d, qh, q, qv ? qs : NULL, qo, qov ? qos : NULL, kh, k,
+                  kv ? ks : NULL, ko, kov ? kos : NULL, a[15] == Py_True ? AMSKV_ROTARY_TRANSPOSED : 0u, stream);
+    Py_END_ALLOW_THREADS
+    PyBuffer_Release(&spec);
+    return PyLong_FromLong(rc);
+}
+
+/* address of a contiguous list of int32: None, an int or a tensor */
+static int list_of(PyObject* x, const int32_t** out)
+{
+    void* p;
+    int64_t s[3];
+    int strided;
+    if (tensor(x, &p, s, &strided) || strided) return -1;
+    *out = (const int32_t*)p;
+    return 0;
+}
+
+/* cross_attend(cache, scale, kv_heads, keys, K, V, Q, out, lengths, offsets, max_keys, stream) -> return code, or None */
+static PyObject* py_cross_attend(PyObject* self, PyObject* const* a, Py_ssize_t n)
+{
+    void *cache, *k, *v, *q, *o, *stream;
+    int64_t ks[3], qs[3], os[3];
+    int scale, kv, qv, ov, rc, heads, keys, max_keys;
+    amskv_encoder enc;
+    if (count(n, 12)) return NULL;
+    if (as_pointer(a[0], &cache) || as_int(a[1], &scale) || as_int(a[2], &heads) || as_int(a[3], &keys) || key_value(a[4], a[5], &k, &v, ks, &kv) ||
+        tensor(a[6], &q, qs, &qv) || tensor(a[7], &o, os, &ov) || list_of(a[8], &enc.lengths) || list_of(a[9], &enc.offsets) ||
+        as_int(a[10], &max_keys) || stream_of(a[11], &stream))
+        return left_to_ctypes();
+    enc.kv_heads = heads;
+    enc.keys = keys;
+    enc.max_keys = max_keys;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f_cross(cache, scale, &enc, k, v, kv ? ks : NULL, q, o, qv ? qs : NULL, ov ? os : NULL, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+/* bind(append, attend, append_attend, rotary, cross_attend): addresses of the library's functions */
 static PyObject* py_bind(PyObject* self, PyObject* const* args, Py_ssize_t n)
 {
-    void* f[3];
-    if (n != 3) {
-        PyErr_SetString(PyExc_TypeError, "bind(append, attend, append_attend)");
+    void* f[5];
+    if (n != 5) {
+        PyErr_SetString(PyExc_TypeError, "bind(append, attend, append_attend, rotary, cross_attend)");
         return NULL;
     }
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < 5; ++i) {
         if (as_pointer(args[i], &f[i]) || !f[i]) {
             PyErr_SetString(PyExc_ValueError, "bind() wants addresses");
             return NULL;
@@ -167,6 +267,8 @@ static PyObject* py_bind(PyObject* self, PyObject* const* args, Py_ssize_t n)
     }
     f_attend = (attend_fn)f[1];
     f_append_attend = (append_attend_fn)f[2];
+    f_rotary = (rotary_fn)f[3];
+    f_cross = (cross_fn)f[4];
     f_append = (append_fn)f[0];
     Py_RETURN_NONE;
 }
@@ -176,6 +278,8 @@ static PyMethodDef methods[] = {
     {"append", (PyCFunction)(void (*)(void))py_append, METH_FASTCALL, NULL},
     {"attend", (PyCFunction)(void (*)(void))py_attend, METH_FASTCALL, NULL},
     {"append_attend", (PyCFunction)(void (*)(void))py_append_attend, METH_FASTCALL, NULL},
+    {"rotary", (PyCFunction)(void (*)(void))py_rotary, METH_FASTCALL, NULL},
+    {"cross_attend", (PyCFunction)(void (*)(void))py_cross_attend, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_steps", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

@@ -28,7 +28,10 @@ def _cross(cache, **change):
     return _code(B.amskv_cross_attend, cache, **args)
 
 
-def test_cross_attention_refuses_bad_arguments():
+@pytest.mark.parametrize("native", [True, False], ids=["native", "ctypes"])
+def test_cross_attention_refuses_bad_arguments(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(B, "_steps", None)
     c = _plan()
     assert _cross(c) == B.ERR_UNSUPPORTED          # all is well, but there is no device memory
     assert _cross(c, keys=1 << 30) == B.ERR_UNSUPPORTED

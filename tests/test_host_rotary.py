@@ -36,7 +36,10 @@ def test_bad_specs_are_refused(spec):
     _refused(B.ERR_INVALID, spec=spec)
 
 
-def test_bad_arguments_are_refused():
+@pytest.mark.parametrize("native", [True, False], ids=["native", "ctypes"])
+def test_bad_arguments_are_refused(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(B, "_steps", None)
     for change in (dict(table=None), dict(table=A + 8), dict(table_rows=0), dict(rows=0), dict(T=0), dict(q_heads=0), dict(k_heads=-1),
                    dict(first=-1), dict(first=13), dict(Q=None), dict(Q=A + 2), dict(Q_out=None), dict(K_out=None), dict(K=None),
                    dict(k_heads=0), dict(index=A + 2), dict(index=A, index_row_stride=-1), dict(head_dim=56)):
@@ -84,3 +87,24 @@ def test_oracle_rotation_is_a_rotation_by_relative_positions(interleaved, axes):
     assert abs(a - b) < 1e-9
     assert np.abs(turn(turn(x, p), p, transposed=True) - x).max() < 1e-12
     assert (turn(x, p)[..., dim:] == x[..., dim:]).all()
+
+
+@pytest.mark.skipif(B._steps is None, reason="the native module is not built")
+def test_what_the_native_module_serves_and_what_it_leaves_to_ctypes():
+    spec, x = B.make_rotary(64), torch.zeros(2, 2, 4, 64, dtype=torch.bfloat16)
+    good = [spec, A, 0, 0, None, None, 2, 4, 64, 2, x, x, 2, x.transpose(0, 1), x.data_ptr(), False, None]   # table_rows 0: refused by the library
+    assert B._steps.rotary(*good) == B.ERR_INVALID
+    idx = torch.zeros(2, 4, dtype=torch.int32)
+    for at, value in ((4, idx), (4, idx[0]), (4, A), (5, 4), (15, True), (16, 0), (13, None)):
+        assert B._steps.rotary(*good[:at], value, *good[at + 1:]) == B.ERR_INVALID, at
+    for at, value in ((0, object()), (0, B.TokenBudget()), (4, idx.t()), (6, 1 << 31), (7, 4.0), (10, x.transpose(2, 3)), (15, 1), (2, "1")):
+        assert B._steps.rotary(*good[:at], value, *good[at + 1:]) is None, at
+    cross = [None, 0, 1, 7, x, x, x, x, None, None, 0, None]
+    assert B._steps.cross_attend(*cross) == B.ERR_INVALID                                                      # no cache
+    for at, value in ((8, idx[0]), (9, A), (11, 0), (4, A)):
+        changed = cross[:at] + [value] + cross[at + 1:]
+        assert B._steps.cross_attend(*changed) == B.ERR_INVALID or at == 4, at
+    for at, value in ((1, 1.0), (3, 1 << 31), (5, x.transpose(0, 1)), (8, idx[:, ::2]), (0, 1.0)):
+        assert B._steps.cross_attend(*cross[:at], value, *cross[at + 1:]) is None, at
+    with pytest.raises(TypeError):
+        B._steps.rotary(spec)
