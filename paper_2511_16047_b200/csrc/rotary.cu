@@ -13,29 +13,56 @@ constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------- the table
 // Entry (n, column) = (cos, sin) of positions[n][axis] * frequency, times the amplitude.  An fp32 angle would be off by 0.06 at position
-// 10^6.  The frequency is a fraction of a turn in 64 bits, the position 24 bits and an exponent: their product, shifted, loses whole turns by
-// wrapping around, which is all the range reduction there is, without a double-precision instruction (their rounding and
-// conversions run at a sixteenth of the rate: 131 071 x 64 27.4 us with them).  What is left, within a quarter turn of a whole or half
-// one, is rounded to fp32 once and goes through sincospif.
-__device__ __forceinline__ float2 table_entry(float position, uint64_t turns, float amplitude)
+// 10^6.  Here the frequency is a fraction of a turn in 64 bits, the position 24 bits and an exponent, and the 64 low bits of their product
+// lose whole turns by wrapping around, which is all the range reduction there is.  The top 32 bits of that, within an eighth of a turn
+// of a quarter, become an fp32 angle (off by 2^-23 of at most pi / 4) for the Taylor sums of sine (to the 9th power: 2e-9 is left) and
+// cosine (to the 10th: 1e-10).  What bounds it is the instructions: 131 071 x 64 entries TABLEUS us, against 10.3 for the table's bytes;
+// with fp64 angles 27.4, with 88-bit products and sincospif 31.2 (95 instructions an entry).
+struct TableRow {   // what a position is, for all its columns
+    uint32_t m, sign;
+    int32_t shift;      // position = +-m * 2^shift
+    bool none;          // not a number or infinite: no angle
+    bool fixed;         // a multiple of 1 / 256 below 2^23, as token numbers are, and then `parts` of them
+    int32_t parts;
+    __device__ __forceinline__ explicit TableRow(float position)
+    {
+        const uint32_t bits = __float_as_uint(position), exponent = (bits >> 23) & 0xffu;
+        m = exponent ? (bits & 0x7fffffu) | 0x800000u : bits & 0x7fffffu;
+        sign = (uint32_t)((int32_t)bits >> 31);
+        shift = (int32_t)max(exponent, 1u) - 150;
+        none = exponent == 255;
+        const float scaled = position * 256.f;
+        fixed = fabsf(scaled) < 2147483648.f && scaled == rintf(scaled);
+        parts = fixed ? (int32_t)scaled : 0;
+    }
+};
+__device__ __forceinline__ float2 table_entry(const TableRow& p, uint64_t turns, float amplitude)
 {
-    const uint32_t bits = __float_as_uint(position), exponent = (bits >> 23) & 0xffu;
-    const uint32_t m = exponent ? (bits & 0x7fffffu) | 0x800000u : bits & 0x7fffffu;
-    const int32_t shift = (exponent ? (int32_t)exponent : 1) - 150;   // position = +-m * 2^shift
-    // m * turns, 88 bits
-    const uint64_t p0 = (uint64_t)m * (uint32_t)turns, p1 = (uint64_t)m * (uint32_t)(turns >> 32), lo = p0 + (p1 << 32);
-    const uint64_t hi = (p1 >> 32) + (lo < p0 ? 1u : 0u);
-    uint64_t phase;   // in 2^-64 turns, whole turns gone
-    if (shift >= 0) phase = shift < 64 ? lo << shift : 0;
-    else if (shift > -64) phase = (lo >> -shift) | (hi << (64 + shift));
-    else phase = shift > -128 ? hi >> (-64 - shift) : 0;
-    const uint32_t x = (uint32_t)((bits >> 31 ? 0ull - phase : phase) >> 32);
-    const uint32_t half = (x + 0x40000000u) >> 31;                    // nearer to half a turn than to a whole one
-    float s, c;
-    sincospif((float)(int32_t)(x ^ (half << 31)) * 4.656612873077393e-10f /* 2^-31 */, &s, &c);
-    float a = half ? -amplitude : amplitude;
-    if (exponent == 255) a = __uint_as_float(0x7fc00000u);            // (no position has no angle)
-    return make_float2(c * a, s * a);
+    // (a right shift leaves out bits of the frequency that the product would bring to less than 2^-32 turns)
+    uint32_t x;   // 2^-32 turns
+    if (p.fixed) {
+        const uint64_t f = turns >> 8;
+        const uint32_t q = (uint32_t)abs(p.parts);
+        x = __umulhi(q, (uint32_t)f) + q * (uint32_t)(f >> 32);
+    } else {
+        const uint64_t f = p.shift >= 0 ? (p.shift < 64 ? turns << p.shift : 0ull) : (p.shift > -64 ? turns >> -p.shift : 0ull);
+        x = __umulhi(p.m, (uint32_t)f) + p.m * (uint32_t)(f >> 32);
+    }
+    x = (x ^ p.sign) - p.sign;
+    const uint32_t quarter = (x + 0x20000000u) >> 30;
+    const float r = (float)(int32_t)(x - (quarter << 30)) * 1.4629180792671596e-09f /* 2 pi / 2^32 */, r2 = r * r;
+    float s = fmaf(r2, 2.7557319e-6f /* 1 / 9! */, -1.9841270e-4f /* 1 / 7! */);
+    s = fmaf(r2, s, 8.3333333e-3f /* 1 / 5! */);
+    s = fmaf(r2, s, -1.6666667e-1f /* 1 / 3! */);
+    s = fmaf(r * r2, s, r);
+    float c = fmaf(r2, -2.7557319e-7f /* 1 / 10! */, 2.4801587e-5f /* 1 / 8! */);
+    c = fmaf(r2, c, -1.3888889e-3f /* 1 / 6! */);
+    c = fmaf(r2, c, 4.1666667e-2f /* 1 / 4! */);
+    c = fmaf(r2, c, -0.5f);
+    c = fmaf(r2, c, 1.f);
+    const float a = p.none ? __uint_as_float(0x7fc00000u) : amplitude;
+    const float cosine = (quarter & 1u ? s : c) * a, sine = (quarter & 1u ? c : s) * a;
+    return make_float2(__uint_as_float(__float_as_uint(cosine) ^ ((quarter + 1u) >> 1 << 31)), __uint_as_float(__float_as_uint(sine) ^ (quarter >> 1 << 31)));
 }
 
 constexpr int kTableRows = 4;   // rows of a thread on their way at a time
@@ -60,9 +87,10 @@ rotary_table_kernel(const float* positions, const __grid_constant__ RotaryFreque
 #pragma unroll
         for (int i = 0; i < kTableRows; ++i) {
             if (row + i * step >= count) break;
+            const TableRow p(pos[i]);
             float2 e[kCols];
 #pragma unroll
-            for (int c = 0; c < kCols; ++c) e[c] = table_entry(pos[i], turns[c], freq.amplitude);
+            for (int c = 0; c < kCols; ++c) e[c] = table_entry(p, turns[c], freq.amplitude);
             float2* dst = table + (row + i * step) * cols + col;
             if constexpr (kCols == 2) *reinterpret_cast<float4*>(dst) = make_float4(e[0].x, e[0].y, e[1].x, e[1].y);
             else dst[0] = e[0];

@@ -1,7 +1,7 @@
 """Rotary positions on the GPU against the definition in 64 bits.
 
-Tolerances.  A table entry: the angle is right to 2^-26 pi (rounded once, in half turns, within a quarter turn), sincospif to two
-units of 2^-24, the amplitude's product to one more: under 2^-21.  An output: three fp32 roundings of |u| + |w| times the amplitude
+Tolerances.  A table entry: the angle, rounded twice, is right to 2^-23 of at most pi / 4, the sums to two units of 2^-24, the
+amplitude's product to one more: under 2^-21.  An output: three fp32 roundings of |u| + |w| times the amplitude
 and the table's error times the same, under 2^-20 of it together, then half a step of bf16, 2^-8 of the value."""
 import numpy as np
 import pytest
@@ -61,6 +61,13 @@ def test_table_of_far_positions_and_a_given_amplitude():
     tol = 2.0 ** -22 + 0.5 * np.abs(angle)[..., None] * 2.0 ** -51
     assert (np.abs(got - want) <= tol)[:4].all()
     assert np.abs(np.linalg.norm(got, axis=-1) - 0.5).max() < 1e-6   # (at 10^15 the angle is lost, not the length)
+
+
+def test_table_of_no_numbers_and_of_the_smallest():
+    pos = torch.tensor([[float("nan")], [float("inf")], [-float("inf")], [1e-45], [-3e-39], [1.17549435e-38], [-0.0]])
+    got = _table(B.make_rotary(8), 8, pos.cuda())[:7].cpu()
+    assert torch.isnan(got[:3]).all()
+    assert (got[3:, :, 0] == 1.0).all() and (got[3:, :, 1].abs() <= 2.0 ** -30).all()
 
 
 def _views(x):
