@@ -62,8 +62,8 @@ struct TilesCfg {
     static constexpr uint32_t kQBytes = kQRows * D * 2, kQHalfBytes = kQRows * 128;
     static constexpr uint32_t kKVBytes = kKT * D * 2, kKVHalfBytes = kKT * 128;
     static constexpr uint32_t kStageBytes = 2 * kKVBytes;
-    static constexpr int kRing = kHeld ? 3 : 0;                 // tiles of codes on their way, each with 32 bytes per warp behind it
-    static constexpr uint32_t kCodeBytes = 2 * kKT * D, kRingBytes = kCodeBytes + kLoadWarps * 32;
+    static constexpr int kRing = kHeld ? 3 : 0;                 // tiles of codes on their way, each with 32 bytes behind it
+    static constexpr uint32_t kCodeBytes = 2 * kKT * D, kRingBytes = kCodeBytes + 32;
     static constexpr uint32_t kSmemBytes = 2048 + 2 * kQBufs * kQBytes + kStages * kStageBytes + kRing * kRingBytes +
                                            (kHeld ? kMaskTab * 8 : 0);   // barriers and slack in front
     static constexpr uint32_t kTmemCols = kWide ? 512 : 256, kSCol = 0, kOCol = 2 * kSBufs * kKT;   // S of both streams, then O of both
@@ -73,32 +73,46 @@ struct TilesCfg {
 };
 
 struct Barriers {
-    uint64_t q_full[2][2], q_free[2][2], kv_full[kMaxStages], kv_empty[kMaxStages], s_full[2][2], p_full[2][2], pv_done[2], o_full[2], drained[2];
+    uint64_t q_full[2][2], q_free[2][2], ring_full[3], ring_empty[3], kv_full[kMaxStages], kv_empty[kMaxStages], s_full[2][2], p_full[2][2], pv_done[2], o_full[2], drained[2];
     uint32_t tmem_base;
     int abort_flag;
 };
 static_assert(sizeof(Barriers) + 1024 <= 2048, "barriers fit in front of the aligned tiles");
 
+// Division of numbers below 2^31 by a launch constant: three instructions where the compiler, not knowing it, takes about twenty.
+struct Divisor {
+    uint32_t d, mul, shift;
+    __host__ void set(int32_t by)
+    {
+        d = (uint32_t)by;
+        for (shift = 0; (1u << shift) < d; ++shift) {}
+        mul = (uint32_t)((((1ull << shift) - d) << 32) / d + 1);
+    }
+    __device__ __forceinline__ int32_t operator()(int32_t n) const { return (int32_t)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+};
 struct TilePlan {
-    int32_t nqt, heads, group, units_per_row;   // query tiles per head; query heads; of them per key/value head; ceil(nqt * heads / 2)
+    Divisor nqt, group, units_per_row;   // query tiles per head; query heads per key/value head; ceil(nqt * heads / 2)
+    int32_t heads;
     int32_t units;
     uint32_t sms;
 };
 // Unit n: streams 2 u and 2 u + 1 of its row's nqt * heads.
 struct Unit {
-    int32_t row, head0, head1, qt0, qt1;
+    int32_t row, head0, head1, qt0, qt1, kv0, kv1;
     bool two, shared;
 
     __device__ __forceinline__ Unit(const TilePlan& p, int32_t n)
     {
-        row = n / p.units_per_row;
-        const int32_t s = 2 * (n - row * p.units_per_row);
-        head0 = s / p.nqt;
-        qt0 = s - head0 * p.nqt;
-        head1 = head0 + (qt0 + 1 == p.nqt ? 1 : 0);
-        qt1 = qt0 + 1 == p.nqt ? 0 : qt0 + 1;
+        row = p.units_per_row(n);
+        const int32_t s = 2 * (n - row * (int32_t)p.units_per_row.d), nqt = (int32_t)p.nqt.d;
+        head0 = p.nqt(s);
+        qt0 = s - head0 * nqt;
+        head1 = head0 + (qt0 + 1 == nqt ? 1 : 0);
+        qt1 = qt0 + 1 == nqt ? 0 : qt0 + 1;
         two = head1 < p.heads;
-        shared = two && head0 / p.group == head1 / p.group;
+        kv0 = p.group(head0);
+        kv1 = two ? p.group(head1) : kv0;
+        shared = two && kv0 == kv1;
     }
     __device__ __forceinline__ int32_t head(int g) const { return g ? head1 : head0; }
     __device__ __forceinline__ int32_t qt(int g) const { return g ? qt1 : qt0; }
@@ -157,6 +171,10 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             mbar_init(smem_u32(&bars->kv_full[s]), kHeld ? C::kLoadWarps : 33);   // (the lanes of the one loading warp, and its bulk copies)
             mbar_init(smem_u32(&bars->kv_empty[s]), C::kMmaWarps);   // one arrival per issuing warp, whether it uses the tile or passes it
         }
+        for (int s = 0; s < C::kRing; ++s) {
+            mbar_init(smem_u32(&bars->ring_full[s]), 1 + kTileBlocks);   // the bulk copies, and a scale word each
+            mbar_init(smem_u32(&bars->ring_empty[s]), C::kLoadWarps);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     // Of a cache's tiles, the same for all units: a bit per slot that holds a key.  (Worked out tile by tile the softmax warps would pay for it:
@@ -192,7 +210,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
     auto unit_at = [&](int32_t n) -> Unit { return Unit(plan, (int32_t)(blockIdx.x + n * gridDim.x)); };
     // the bounds of unit n's row, asked for a unit ahead (those of the last unit once more behind it)
     auto bounds_at = [&](int32_t n) -> EncoderBounds {
-        return EncoderBounds(enc, (int32_t)(blockIdx.x + min(n, n_units - 1) * gridDim.x) / plan.units_per_row);
+        return EncoderBounds(enc, plan.units_per_row((int32_t)(blockIdx.x + min(n, n_units - 1) * gridDim.x)));
     };
     // S buffer and phase of a stream's tile t; query buffer and phase of its unit n
     auto buf_of = [](uint32_t t) -> uint32_t { return C::kSBufs == 2 ? t & 1u : 0u; };
@@ -252,10 +270,9 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             EncoderBounds ahead = bounds_at(0);
             for (int32_t n = 0; ok && n < n_units; ++n) {
                 const Unit u = unit_at(n);
-                const EncoderView view(enc, u.row, u.head0 / plan.group, ahead);
+                const EncoderView view(enc, u.row, u.kv0, ahead);
                 const int32_t first_key = ahead.first(enc);
                 ahead = bounds_at(n + 1);
-                const int32_t kv0 = u.head0 / plan.group, kv1 = u.two ? u.head1 / plan.group : kv0;
                 const int32_t blocks = view.blocks();
                 const int n_tiles = (blocks + kTileBlocks - 1) / kTileBlocks, per_tile = u.two && !u.shared ? 2 : 1;
                 if (C::kLoaderQ && n_tiles > 0) {
@@ -282,7 +299,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                         const int whole = min(left / kBlock, kTileBlocks), over = left - whole * kBlock;   // blocks of values; values over (>= 16: none)
                         if (elect_one()) {
                             mbar_expect_tx(bar, C::kKVBytes + (uint32_t)whole * kBlock * D * 2);
-                            const int tok = first_key + j * kKT, head = g ? kv1 : kv0, from = enc.row_maps ? u.row : 0;
+                            const int tok = first_key + j * kKT, head = g ? u.kv1 : u.kv0, from = enc.row_maps ? u.row : 0;
                             const int3 c = coords(kpos, tok, head, from);
 #pragma unroll
                             for (int h = 0; h < C::kHalves; ++h) tma_load_4d(dst + h * C::kKVHalfBytes, &k_map, bar, h * 64, c.x, c.y, c.z);
@@ -302,7 +319,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                         }
                         __syncwarp();
                         if (whole < kTileBlocks && over > 0) {
-                            const __nv_bfloat16* src = view.v + (int64_t)(j * kKT + whole * kBlock) * view.tok + (g ? (int64_t)(kv1 - kv0) * enc.head : 0) + piece * 8;
+                            const __nv_bfloat16* src = view.v + (int64_t)(j * kKT + whole * kBlock) * view.tok + (g ? (int64_t)(u.kv1 - u.kv0) * enc.head : 0) + piece * 8;
 #pragma unroll
                             for (int i = 0; i < kBlock / kRows; ++i) {
                                 const int r = i * kRows + row;
@@ -316,6 +333,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                         ++issued;
                         next_stage();
                     }
+
                 }
             }
             // whatever becomes of the launch, copies into shared memory end before the CTA does
@@ -329,9 +347,11 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     for (uint32_t q = q_asked[g] > 2u ? q_asked[g] - 2u : 0u; q < q_asked[g]; ++q) await_q(g, q);
             }
         } else {
-            // Codes land in a ring of their own, each lane's where it will take them from again, and what belongs to the tile in 32 bytes of the
-            // warp: the scale words of its four blocks and the slots that the products read (0: there is no further tile).  (With the
-            // codes fetched into registers instead, a wait for a tile's waits for all younger ones too, as loads are counted, not named.)
+            // Codes land in a ring of their own by bulk copies of whole blocks, asked for by the first warp, and with them the scale words of the
+            // four blocks and the number of slots that the products read (0: there is no further tile).  Slots without a key keep what
+            // they held: any code is a finite number, and its probability is zero.  (Fetched into registers instead, a wait for a tile's codes
+            // waits for all younger ones too, as loads are counted, not named; with 16-byte copies of every lane the copies took as
+            // many instructions as the widening.)
             using Share = CodeShare<D>;
             // A lane's piece and row of a pass.  The row's lowest bit is bit 2 of the lane, so that eight lanes that store together, four pieces of two
             // rows, meet all banks.
@@ -346,43 +366,70 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             const int n_tiles = (held.blocks + kTileBlocks - 1) / kTileBlocks;
             uint8_t* ring = smem_raw + (kv_smem - raw) + C::kStages * C::kStageBytes;
             const uint32_t ring_at = kv_smem + C::kStages * C::kStageBytes;
+            const uint32_t ring_full0 = smem_u32(&bars->ring_full[0]), ring_empty0 = smem_u32(&bars->ring_empty[0]);
             int32_t f_n = 0;   // the walk of the copies: unit, tile, stream
             int f_j = 0, f_g = 0;
             Unit f_u = unit_at(0);
             HeldView view(held, (int64_t)f_u.row * plan.heads + f_u.head0, D);
             const int64_t values_at = (int64_t)held.capacity * D, codes_of_item = 2 * values_at, scales_of_item = held.capacity / kBlock;
-            int32_t pos[kTileBlocks] = {}, valid[kTileBlocks] = {};   // blocks of tile f_j
-            auto fetch = [&](uint32_t slot) {
-                const uint32_t at = slot * C::kRingBytes, words = at + C::kCodeBytes + w * 32;
+            uint32_t f_slot = 0, f_phase = 0, asked = 0;
+            bool ended = false;
+            auto fetch = [&]() -> bool {   // (the first warp) the next tile into the ring
+                if (ended) return true;
+                if (!warp_wait(ring_empty0 + 8 * f_slot, f_phase ^ 1u, abort_flag)) return false;
+                const uint32_t at = f_slot * C::kRingBytes, bar = ring_full0 + 8 * f_slot;
+                int* slots = reinterpret_cast<int*>(ring + at + C::kCodeBytes + 16);
                 if (f_n >= n_units) {
-                    if (lane == 0) *reinterpret_cast<int*>(ring + words + 16) = 0;
-                    asm volatile("cp.async.commit_group;" ::: "memory");
-                    return;
+                    ended = true;
+                    if (lane == 0) {
+                        *slots = 0;
+                        mbar_arrive_n(bar, 1 + kTileBlocks);
+                    }
+                    __syncwarp();
+                    ++asked;   // (it takes a phase of its place, as a tile does)
+                    return true;
                 }
                 const int32_t b0 = f_j * kTileBlocks;
-                if (f_g == 0) {
-                    const bool whole = view.whole4(b0);
-                    pos[0] = view.position(b0);
-#pragma unroll
-                    for (int b = 0; b < kTileBlocks; ++b) {
-                        valid[b] = whole ? kBlock : view.valid(b0 + b);
-                        pos[b] = whole ? pos[0] + b * kBlock : valid[b] > 0 ? view.position(b0 + b) : 0;
+                const bool whole = view.whole4(b0);
+                const int32_t first = view.position(b0);
+                if (lane < kTileBlocks) {   // (a block that is not there: the first one's word)
+                    int32_t p = first + lane * kBlock;
+                    if (!whole) {
+                        HeldView own = view;
+                        p = own.valid(b0 + lane) > 0 ? own.position(b0 + lane) : first;
+                    }
+                    copy4(ring_at + at + C::kCodeBytes + lane * 4, view.scales + (f_g ? scales_of_item : 0) + p / kBlock);
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+                }
+                if (lane == 0) {
+                    const uint8_t* codes = view.codes + (f_g ? codes_of_item : 0);
+                    *slots = min(kTileBlocks, held.blocks - b0) * kBlock;
+                    if (whole) {
+                        mbar_expect_tx(bar, C::kCodeBytes);
+                        bulk_load(ring_at + at, codes + (int64_t)first * D, kKT * D, bar);
+                        bulk_load(ring_at + at + kKT * D, codes + values_at + (int64_t)first * D, kKT * D, bar);
+                    } else {
+                        HeldView count = view, own = view;
+                        uint32_t bytes = 0;
+#pragma unroll 1
+                        for (int b = 0; b < kTileBlocks; ++b) bytes += 2u * count.valid(b0 + b) * D;
+                        mbar_expect_tx(bar, bytes);
+#pragma unroll 1
+                        for (int b = 0; b < kTileBlocks; ++b) {
+                            const uint32_t n = own.valid(b0 + b) * D;
+                            if (n == 0) break;
+                            const uint8_t* src = codes + (int64_t)own.position(b0 + b) * D;
+                            bulk_load(ring_at + at + b * kBlock * D, src, n, bar);
+                            bulk_load(ring_at + at + (kKT + b * kBlock) * D, src + values_at, n, bar);
+                        }
                     }
                 }
-                const uint8_t* codes = view.codes + (f_g ? codes_of_item : 0) + row * D + piece * 16;
-#pragma unroll
-                for (int i = 0; i < Share::kN; ++i) {
-                    const int b = i * Share::kWarps * Share::kRows % kKT / kBlock;   // (the same for all warps)
-                    const int p = w + i * Share::kWarps, first = p * Share::kRows % kBlock;
-                    copy16_or_zero(ring_at + at + (p * 32 + lane) * 16, codes + (i >= Share::kN / 2 ? values_at : 0) + (int64_t)(pos[b] + first) * D,
-                                   first + row < valid[b]);
+                __syncwarp();
+                ++asked;
+                if (++f_slot == C::kRing) {
+                    f_slot = 0;
+                    f_phase ^= 1u;
                 }
-                if (lane < kTileBlocks) {
-                    const int32_t mine = lane == 0 ? pos[0] : lane == 1 ? pos[1] : lane == 2 ? pos[2] : pos[3];
-                    copy4(ring_at + words + lane * 4, view.scales + (f_g ? scales_of_item : 0) + mine / kBlock);   // (block 0's for one that is not there)
-                }
-                if (lane == 0) *reinterpret_cast<int*>(ring + words + 16) = min(kTileBlocks, held.blocks - b0) * kBlock;
-                asm volatile("cp.async.commit_group;" ::: "memory");
                 // next: the other stream's tile (the item behind this one), the next tile, the next unit
                 if (f_u.two && !f_u.shared && f_g == 0) {
                     f_g = 1;
@@ -396,24 +443,26 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                         }
                     }
                 }
+                return true;
             };
-            uint32_t slot = 0;   // of the next tile
-            for (uint32_t i = 0; i + 1 < C::kRing; ++i) fetch(i);
-            for (;;) {
-                __syncwarp();    // all lanes have taken the tile before out of the ring
-                fetch(slot == 0 ? C::kRing - 1 : slot - 1);
-                asm volatile("cp.async.wait_group %0;" ::"n"(C::kRing - 1) : "memory");
-                __syncwarp();    // (the words are other lanes' copies)
+            uint32_t slot = 0, ring_phase = 0;   // of the next tile
+            if (w == 0)
+                for (int i = 0; ok && i < C::kRing; ++i) ok = fetch();
+            while (ok) {
+                if (!warp_wait(ring_full0 + 8 * slot, ring_phase, abort_flag)) {
+                    ok = false;
+                    break;
+                }
                 const uint8_t* from = ring + slot * C::kRingBytes;
-                const int rows = *reinterpret_cast<const int*>(from + C::kCodeBytes + w * 32 + 16);
+                const int rows = *reinterpret_cast<const int*>(from + C::kCodeBytes + 16);
                 if (rows == 0) break;
-                const uint4 words = *reinterpret_cast<const uint4*>(from + C::kCodeBytes + w * 32);
+                const uint4 words = *reinterpret_cast<const uint4*>(from + C::kCodeBytes);
                 if (!free_stage()) {
                     ok = false;
                     break;
                 }
                 uint8_t* dst = smem_raw + (kv_smem - raw) + stage * C::kStageBytes;
-                const uint8_t* mine = from + (w * 32 + lane) * 16;
+                const uint8_t* mine = from + (w * Share::kRows + row) * D + piece * 16;
                 auto put = [&](int i, const uint4& codes, uint32_t factor, uint32_t rest) {
                     const int p = w + i * Share::kWarps;
                     uint4 lo, hi;
@@ -421,7 +470,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     *reinterpret_cast<uint4*>(dst + at_pass(part_lo, p)) = lo;
                     *reinterpret_cast<uint4*>(dst + at_pass(part_hi, p)) = hi;
                 };
-                auto codes_at = [&](int i) -> uint4 { return *reinterpret_cast<const uint4*>(mine + i * Share::kWarps * 512); };
+                auto codes_at = [&](int i) -> uint4 { return *reinterpret_cast<const uint4*>(mine + i * Share::kWarps * Share::kRows * D); };
                 if (rows == kKT && ((words.x | words.y | words.z | words.w) >> 16) == 0u) {
                     // (nearly always) several passes' codes before the first is stored: no load can move above a store for the compiler
 #pragma unroll
@@ -444,11 +493,22 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     }
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(kv_full0 + 8 * stage);
+                if (lane == 0) {
+                    mbar_arrive(kv_full0 + 8 * stage);
+                    mbar_arrive(ring_empty0 + 8 * slot);
+                }
                 next_stage();
-                slot = slot + 1 == C::kRing ? 0 : slot + 1;
+                if (++slot == C::kRing) {
+                    slot = 0;
+                    ring_phase ^= 1u;
+                }
+                if (w == 0) ok = fetch();   // into the place of this tile, or of one that other warps are still at: two are there meanwhile
             }
+            // whatever becomes of the launch, copies into shared memory end before the CTA does
             asm volatile("cp.async.wait_all;" ::: "memory");
+            for (uint32_t q = asked > (uint32_t)C::kRing ? asked - C::kRing : 0u; q < asked; ++q)
+                for (uint32_t i = 0; i < kSpinLimit; ++i)
+                    if (mbar_try_wait(ring_full0 + 8 * (q % C::kRing), (q / C::kRing) & 1u)) break;
         }
         if (!ok && lane == 0) report(status, kStatusTmaTimeout, abort_flag);
     } else if (warp >= mma_warp && warp < mma_warp + C::kMmaWarps) {
@@ -828,15 +888,15 @@ cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, c
 {
     using C = TilesCfg<D, kHeld>;
     TilePlan plan;
+    const int32_t nqt = (T + kQRows - 1) / kQRows;
     plan.heads = kv_heads * group;
-    plan.group = group;
     plan.sms = (uint32_t)sm_count;
-    plan.nqt = (T + kQRows - 1) / kQRows;
-    const int64_t streams = (int64_t)plan.nqt * plan.heads;
-    if (T < 1 || streams > 0x7ffffffell) return cudaErrorInvalidValue;
-    plan.units_per_row = (int32_t)((streams + 1) / 2);
-    if ((int64_t)rows * plan.units_per_row > 0x3fffffffll) return cudaErrorInvalidValue;   // (indices one round of CTAs beyond are formed)
-    plan.units = rows * plan.units_per_row;
+    const int64_t streams = (int64_t)nqt * plan.heads, per_row = (streams + 1) / 2;
+    if (T < 1 || (int64_t)rows * per_row > 0x3fffffffll) return cudaErrorInvalidValue;   // (indices one round of CTAs beyond are formed)
+    plan.nqt.set(nqt);
+    plan.group.set(group);
+    plan.units_per_row.set((int32_t)per_row);
+    plan.units = (int32_t)(rows * per_row);
     CUtensorMap qm;
     int pos[3];
     if (!tc_encode_q_map(Q, T, rows, plan.heads, D, kQRows, &qm, pos)) return cudaErrorNotSupported;
