@@ -42,7 +42,7 @@ constexpr int kMmaWarp = 8;
 constexpr int kMaxStages = 4;
 constexpr float kRescaleLog2 = 8.f;
 constexpr float kSumLimit = 1.8446744e19f;   // 2^64
-constexpr int kMaskTab = 192;                // tiles of a cache whose masks are tabulated in shared memory
+constexpr int kHeldTab = 192;                // tiles of a cache that are tabulated in shared memory
 
 template <int D, bool kHeld>
 struct TilesCfg {
@@ -56,7 +56,8 @@ struct TilesCfg {
     // 64 channels costs more than scattered stores do.
     static constexpr bool kBulkOut = kWide;
     static constexpr int kMmaWarps = kWide ? 2 : 1, kLoadWarps = kWide && kHeld ? 4 : 1;
-    static constexpr int kWarps = kMmaWarp + kMmaWarps + kLoadWarps, kThreads = kWarps * 32;
+    static constexpr int kFetchWarps = kWide && kHeld ? 1 : 0;  // a warp that only asks for codes, else the first loading warp does
+    static constexpr int kWarps = kMmaWarp + kMmaWarps + kLoadWarps + kFetchWarps, kThreads = kWarps * 32;
     static constexpr bool kLoaderQ = kQBufs == 2;               // the loading warp fetches the queries, else a lane of each softmax group does
     static constexpr int kHalves = D / 64;                      // 128-byte swizzle atoms per row
     static constexpr uint32_t kQBytes = kQRows * D * 2, kQHalfBytes = kQRows * 128;
@@ -65,7 +66,7 @@ struct TilesCfg {
     static constexpr int kRing = kHeld ? 3 : 0;                 // tiles of codes on their way, each with 32 bytes behind it
     static constexpr uint32_t kCodeBytes = 2 * kKT * D, kRingBytes = kCodeBytes + 32;
     static constexpr uint32_t kSmemBytes = 2048 + 2 * kQBufs * kQBytes + kStages * kStageBytes + kRing * kRingBytes +
-                                           (kHeld ? kMaskTab * 8 : 0);   // barriers and slack in front
+                                           (kHeld ? kHeldTab * 24 : 0);   // barriers and slack in front
     static constexpr uint32_t kTmemCols = kWide ? 512 : 256, kSCol = 0, kOCol = 2 * kSBufs * kKT;   // S of both streams, then O of both
     static_assert(kOCol + 2 * D <= kTmemCols && kCtasPerSm * kTmemCols <= 512, "tensor memory");
     static_assert(kCtasPerSm * (kSmemBytes + 1024) <= 228 * 1024, "shared memory");
@@ -134,6 +135,23 @@ __device__ __forceinline__ int3 coords(const int3& pos, int tok, int head, int r
     return make_int3(at(1), at(2), at(3));
 }
 
+// Tile j of a cache: a bit per slot that holds a key, and the first slots of the blocks.  (Not inlined: beyond the table it is hardly ever
+// called, and the registers are the softmax warps'.)
+__device__ __noinline__ uint64_t held_tile(const HeldKeys& held, int j, int4* pos)
+{
+    HeldView view(held, 0, 0);
+    uint64_t keep = 0;
+    int32_t p[kTileBlocks];
+#pragma unroll
+    for (int b = 0; b < kTileBlocks; ++b) {
+        const int32_t n = view.valid(j * kTileBlocks + b);
+        keep |= ((1ull << n) - 1ull) << (b * kBlock);
+        p[b] = n > 0 ? view.position(j * kTileBlocks + b) : p[0];   // (the first block is there)
+    }
+    if (pos) *pos = make_int4(p[0], p[1], p[2], p[3]);
+    return keep;
+}
+
 template <int D, bool kHeld>
 __global__ void __launch_bounds__(TilesCfg<D, kHeld>::kThreads, TilesCfg<D, kHeld>::kCtasPerSm)
 attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const __grid_constant__ CUtensorMap o_map, int3 opos,
@@ -177,20 +195,12 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    // Of a cache's tiles, the same for all units: a bit per slot that holds a key.  (Worked out tile by tile the softmax warps would pay for it:
-    // 430 keys x 256 queries x 3 840 heads of 64 311 us, 246 without.)
-    auto mask_of = [](HeldView& view, int j) -> uint64_t {
-        if (view.whole4(j * kTileBlocks)) return ~0ull;
-        uint64_t keep = 0;
-#pragma unroll
-        for (int b = 0; b < kTileBlocks; ++b) keep |= ((1ull << view.valid(j * kTileBlocks + b)) - 1ull) << (b * kBlock);
-        return keep;
-    };
-    uint64_t* mask_tab = reinterpret_cast<uint64_t*>(smem_raw + (kv_smem - raw) + C::kStages * C::kStageBytes + C::kRing * C::kRingBytes);
-    if (kHeld) {
-        HeldView view(held, 0, D);
-        for (int j = threadIdx.x; j < kMaskTab && j * kTileBlocks < held.blocks; j += C::kThreads) mask_tab[j] = mask_of(view, j);
-    }
+    // A cache's tiles, the same for all units, are tabulated: worked out tile by tile the softmax and the loading warps would pay for it (430 keys x
+    // 256 queries x 3 840 heads of 64: 311 us, 246 with the masks in a table, 232 with the positions, too).
+    int4* pos_tab = reinterpret_cast<int4*>(smem_raw + (kv_smem - raw) + C::kStages * C::kStageBytes + C::kRing * C::kRingBytes);
+    uint64_t* mask_tab = reinterpret_cast<uint64_t*>(pos_tab + kHeldTab);
+    if (kHeld)
+        for (int j = threadIdx.x; j < kHeldTab && j * kTileBlocks < held.blocks; j += C::kThreads) mask_tab[j] = held_tile(held, j, pos_tab + j);
     if (warp == kMmaWarp) {
         __syncwarp();
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem_base)), "r"(C::kTmemCols)
@@ -238,7 +248,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             if (mbar_try_wait(q_full0 + 16 * g + 8 * qbuf_of(q), qpar_of(q))) break;
     };
 
-    if (warp >= load_warp && warp < load_warp + C::kLoadWarps) {
+    if (warp >= load_warp && warp < load_warp + C::kLoadWarps + C::kFetchWarps) {
         // ------------------------------------------------------------ key/value stages
         uint32_t stage = 0, phase = 0;   // of the next tile
         bool ok = true;
@@ -347,7 +357,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     for (uint32_t q = q_asked[g] > 2u ? q_asked[g] - 2u : 0u; q < q_asked[g]; ++q) await_q(g, q);
             }
         } else {
-            // Codes land in a ring of their own by bulk copies of whole blocks, asked for by the first warp, and with them the scale words of the
+            // Codes land in a ring of their own by bulk copies of whole blocks, and with them the scale words of the
             // four blocks and the number of slots that the products read (0: there is no further tile).  Slots without a key keep what
             // they held: any code is a finite number, and its probability is zero.  (Fetched into registers instead, a wait for a tile's codes
             // waits for all younger ones too, as loads are counted, not named; with 16-byte copies of every lane the copies took as
@@ -370,11 +380,11 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             int32_t f_n = 0;   // the walk of the copies: unit, tile, stream
             int f_j = 0, f_g = 0;
             Unit f_u = unit_at(0);
-            HeldView view(held, (int64_t)f_u.row * plan.heads + f_u.head0, D);
-            const int64_t values_at = (int64_t)held.capacity * D, codes_of_item = 2 * values_at, scales_of_item = held.capacity / kBlock;
+            const int64_t values_at = (int64_t)held.capacity * D, scales_of_item = held.capacity / kBlock;
             uint32_t f_slot = 0, f_phase = 0, asked = 0;
             bool ended = false;
-            auto fetch = [&]() -> bool {   // (the first warp) the next tile into the ring
+            static_assert(C::kFetchWarps == 1 || C::kLoadWarps == 1, "one warp asks for codes");
+            auto fetch = [&]() -> bool {   // the next tile into the ring
                 if (ended) return true;
                 if (!warp_wait(ring_empty0 + 8 * f_slot, f_phase ^ 1u, abort_flag)) return false;
                 const uint32_t at = f_slot * C::kRingBytes, bar = ring_full0 + 8 * f_slot;
@@ -389,39 +399,31 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     ++asked;   // (it takes a phase of its place, as a tile does)
                     return true;
                 }
-                const int32_t b0 = f_j * kTileBlocks;
-                const bool whole = view.whole4(b0);
-                const int32_t first = view.position(b0);
-                if (lane < kTileBlocks) {   // (a block that is not there: the first one's word)
-                    int32_t p = first + lane * kBlock;
-                    if (!whole) {
-                        HeldView own = view;
-                        p = own.valid(b0 + lane) > 0 ? own.position(b0 + lane) : first;
-                    }
-                    copy4(ring_at + at + C::kCodeBytes + lane * 4, view.scales + (f_g ? scales_of_item : 0) + p / kBlock);
-                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+                int4 pos;
+                uint64_t keep;
+                if (f_j < kHeldTab) {
+                    pos = pos_tab[f_j];
+                    keep = mask_tab[f_j];
+                } else {
+                    keep = held_tile(held, f_j, &pos);
                 }
+                const int64_t item = (int64_t)f_u.row * plan.heads + f_u.head0 + f_g;   // (the other stream's is the item behind the first one's)
+                const uint8_t* codes = held.codes + item * 2 * values_at;
+                const uint32_t to = ring_at + at;
                 if (lane == 0) {
-                    const uint8_t* codes = view.codes + (f_g ? codes_of_item : 0);
-                    *slots = min(kTileBlocks, held.blocks - b0) * kBlock;
-                    if (whole) {
-                        mbar_expect_tx(bar, C::kCodeBytes);
-                        bulk_load(ring_at + at, codes + (int64_t)first * D, kKT * D, bar);
-                        bulk_load(ring_at + at + kKT * D, codes + values_at + (int64_t)first * D, kKT * D, bar);
-                    } else {
-                        HeldView count = view, own = view;
-                        uint32_t bytes = 0;
-#pragma unroll 1
-                        for (int b = 0; b < kTileBlocks; ++b) bytes += 2u * count.valid(b0 + b) * D;
-                        mbar_expect_tx(bar, bytes);
-#pragma unroll 1
-                        for (int b = 0; b < kTileBlocks; ++b) {
-                            const uint32_t n = own.valid(b0 + b) * D;
-                            if (n == 0) break;
-                            const uint8_t* src = codes + (int64_t)own.position(b0 + b) * D;
-                            bulk_load(ring_at + at + b * kBlock * D, src, n, bar);
-                            bulk_load(ring_at + at + (kKT + b * kBlock) * D, src + values_at, n, bar);
-                        }
+                    *slots = min(kTileBlocks, held.blocks - f_j * kTileBlocks) * kBlock;
+                    mbar_expect_tx(bar, 2u * (uint32_t)__popcll(keep) * D);
+                }
+                __syncwarp();
+                if (lane < kTileBlocks) {   // a lane per block (one that is not there: the first one's word)
+                    const int32_t p = lane == 0 ? pos.x : lane == 1 ? pos.y : lane == 2 ? pos.z : pos.w;
+                    copy4(to + C::kCodeBytes + lane * 4, held.scales + item * scales_of_item + p / kBlock);
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+                    const bool whole = keep == ~0ull && pos.w == pos.x + 3 * kBlock;   // one piece of the region (blocks are in its order)
+                    const uint32_t n = whole ? (lane == 0 ? (uint32_t)kKT : 0u) : (uint32_t)__popcll((keep >> (lane * kBlock)) & 0xffffull);
+                    if (n > 0) {
+                        bulk_load(to + lane * kBlock * D, codes + (int64_t)p * D, n * D, bar);
+                        bulk_load(to + (kKT + lane * kBlock) * D, codes + values_at + (int64_t)p * D, n * D, bar);
                     }
                 }
                 __syncwarp();
@@ -437,18 +439,17 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     f_g = 0;
                     if (++f_j == n_tiles) {
                         f_j = 0;
-                        if (++f_n < n_units) {
-                            f_u = unit_at(f_n);
-                            view.restart(held, (int64_t)f_u.row * plan.heads + f_u.head0, D);
-                        }
+                        if (++f_n < n_units) f_u = unit_at(f_n);
                     }
                 }
                 return true;
             };
             uint32_t slot = 0, ring_phase = 0;   // of the next tile
-            if (w == 0)
+            if (C::kFetchWarps > 0 && w == C::kLoadWarps)
+                while (ok && !ended) ok = fetch();
+            if (C::kFetchWarps == 0)
                 for (int i = 0; ok && i < C::kRing; ++i) ok = fetch();
-            while (ok) {
+            while (ok && w < C::kLoadWarps) {
                 if (!warp_wait(ring_full0 + 8 * slot, ring_phase, abort_flag)) {
                     ok = false;
                     break;
@@ -502,7 +503,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     slot = 0;
                     ring_phase ^= 1u;
                 }
-                if (w == 0) ok = fetch();   // into the place of this tile, or of one that other warps are still at: two are there meanwhile
+                if (C::kFetchWarps == 0) ok = fetch();   // into the place of this tile
             }
             // whatever becomes of the launch, copies into shared memory end before the CTA does
             asm volatile("cp.async.wait_all;" ::: "memory");
@@ -678,11 +679,10 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     const int groups = min(kTileBlocks, blocks - j * kTileBlocks);
                     uint64_t keep = ~0ull;   // a bit per column that holds a key
                     if (kHeld) {
-                        if (j < kMaskTab) {
+                        if (j < kHeldTab) {
                             keep = mask_tab[j];
                         } else {
-                            HeldView view(held, 0, D);
-                            keep = mask_of(view, j);
+                            keep = held_tile(held, j, nullptr);
                         }
                     } else if (len - j * kKT < kKT) {
                         keep = (1ull << (len - j * kKT)) - 1ull;

@@ -61,13 +61,6 @@ struct HeldView {
     {
         n = (ranges.r[0].len + kBlock - 1) / kBlock;
     }
-    __device__ __forceinline__ void restart(const HeldKeys& h, int64_t item, int32_t D)   // the same ranges of another item
-    {
-        codes = h.codes + item * 2 * h.capacity * D;
-        scales = h.scales + item * (h.capacity / kBlock);
-        range = first = 0;
-        n = (ranges.r[0].len + kBlock - 1) / kBlock;
-    }
     __device__ __forceinline__ int32_t blocks() const { return total; }
     __device__ __forceinline__ void walk(int32_t b)
     {
@@ -82,12 +75,6 @@ struct HeldView {
         if (b >= total) return 0;
         walk(b);
         return min(ranges.r[range].len - (b - first) * kBlock, kBlock);
-    }
-    __device__ __forceinline__ bool whole4(int32_t b)   // blocks b .. b + 3 are full, and of one range
-    {
-        if (b + 3 >= total) return false;
-        walk(b);
-        return b + 4 - first <= ranges.r[range].len / kBlock;
     }
     __device__ __forceinline__ int32_t position(int32_t b)   // first slot of block b < total
     {
