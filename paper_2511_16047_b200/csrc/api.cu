@@ -272,11 +272,11 @@ void note_appended(amskv_cache* cache, int layer, int scale)
 // between them, and where 16 rows or fewer leave the other's tiles of 128 empty.  `items`: rows x key/value heads; `group` query heads share one.
 // us per call, warp-matrix / tensor-memory, in a graph, 256 keys where nothing else is said:
 //   64 channels, an encoder:   T = 16  512 items 6.6 / 10.2, 8 192 88 / 99 (77 keys 67 / 60);  T = 36  128 6.3 / 8.9, 512 11.8 / 10.6;
-//     T = 100  128 (two CTAs each) 8.4 / 9.5, 512 24.5 / 12.4;  T = 144  32 8.9 / 12.3, 128 (three) 13.0 / 10.2;  T = 576  32 10.1 / 10.8
+//     T = 100  128 8.2 / 9.0, 512 24.5 / 12.4;  T = 144  32 4.6 / 8.5, 128 11.1 / 8.7;  T = 256  32 5.7 / 9.0, 64 8.2 / 9.0
 //   64 channels, 8 bits:       T = 36  512 14.2 / 16.1, 2 048 53 / 56;  T = 64  2 048 60 / 62, 8 192 219 / 204;  T = 100  128 10.3 / 14.9, 512 29.8 / 17.2
 //   128 channels, an encoder:  T = 16  512 12.2 / 16.5, 8 192 184 / 205 (77 keys 127 / 111);  T = 64  128 9.3 / 9.6 (512 keys 15.0 / 13.5, 1 024 21.5 / 23.5),
-//     512 26.2 / 17.5;  T = 100  32 10.3 / 10.9, 128 (two CTAs each) 11.9 / 10.0;  T = 144  32 13.2 / 12.9
-//   128 channels, 8 bits:      T = 36  128 12.3 / 12.6, 512 30.4 / 23.8;  T = 100  32 11.2 / 12.8, 128 15.7 / 13.1;  T = 144  32 13.4 / 11.9
+//     512 26.2 / 17.5;  T = 100  32 6.7 / 9.3, 64 8.5 / 9.3;  T = 144  16 5.1 / 8.2, 32 6.7 / 8.2, 64 11.5 / 8.5;  T = 256  16 6.7 / 8.9, 32 8.5 / 9.0
+//   128 channels, 8 bits:      T = 36  128 14.0 / 13.1, 512 30.4 / 23.8;  T = 100  32 13.3 / 15.4, 128 21.1 / 15.7;  T = 144  16 12.6 / 12.3, 32 14.8 / 12.5
 bool takes_tiles(const amskv_cache* cache, int32_t T, int32_t group, int64_t items, int64_t keys)
 {
     if (!cache->tc_ready || cache->path == AMSKV_PATH_SMALL || cache->path == AMSKV_PATH_SIMT) return false;
@@ -285,7 +285,7 @@ bool takes_tiles(const amskv_cache* cache, int32_t T, int32_t group, int64_t ite
     if (M <= 16) return items > 16 * sms && keys <= 256;
     if (M <= 32 && items <= 4 * sms) return false;
     if (cache->head_dim == 64) return ctas > 2 * sms && !(cache->held() && M <= 64 && items <= 16 * sms);
-    return M > 128 || ctas > sms;
+    return ctas > sms || (M > 128 && (cache->held() || items * ((M + 15) / 16) > 2 * sms));
 }
 
 // which kernel amskv_attend uses for T query tokens over `total` keys

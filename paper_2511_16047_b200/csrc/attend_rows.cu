@@ -406,13 +406,13 @@ cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, c
     const cudaError_t oe = opt_in.ensure(attend_rows_kernel<D, kQB, kHeld>, C::kSmemBytes);
     if (oe != cudaSuccess) return oe;
     const int64_t blocks = ((int64_t)T * group + 15) / 16, parts = (blocks + kQB - 1) / kQB, ctas = parts * rows * kv_heads;
-    // Few CTAs and several chunks of keys: clusters share them.
-    // A merge of 64 rows costs what several chunks do, of codes fewer (128 channels, 32 items, 256 keys, shared from 4 chunks a CTA / from 8:
-    // T = 16 6.7 / -, T = 36 9.8 / 9.7, T = 144 14.6 / 13.2; 8 bits, T = 36 9.7 / 12.0 us; two chunks are not shared: T = 16, 77 keys 4.4 / 6.3).
-    constexpr int kMinChunks = kQB == 4 && !kHeld ? 8 : 4;
+    // Few CTAs and several chunks of keys: clusters share them.  What a merge costs is about four chunks of an encoder's keys (in CTAs of
+    // 64 rows more) or two of codes (256 keys in four chunks, shared by two CTAs / not: 64 channels 5.4 / 4.6, 128 channels 7.5 / 6.7 us;
+    // 484 keys 6.2 / 6.7 and 9.0 / 9.8; 8 bits, 64 channels, 256 keys 6.2 / 7.6).
+    constexpr int kFirst = kHeld ? 4 : 8, kMore = kQB == 4 && !kHeld ? 8 : 4;
     const int64_t chunks = (max_keys + kChunk - 1) / kChunk;
     int32_t splits = 1;
-    while (splits < 8 && ctas * splits * 2 <= 2ll * sm_count && chunks >= splits * kMinChunks) splits *= 2;
+    while (splits < 8 && ctas * splits * 2 <= 2ll * sm_count && chunks >= (splits == 1 ? kFirst : splits * kMore)) splits *= 2;
     if (ctas * splits > 0x7fffffffll) return cudaErrorInvalidValue;
     return launch_kernel(true, attend_rows_kernel<D, kQB, kHeld>, dim3((unsigned)(ctas * splits)), dim3(kThreads),
                          KernelMemory(C::kSmemBytes, (unsigned)splits), stream, (const __nv_bfloat16*)Q.ptr, Q.row, Q.head, Q.token,
@@ -428,13 +428,22 @@ cudaError_t launch_any(const Strided& Q, const Strided& O, const EncoderKeys& en
     const float scale_log2 = softmax_scale * 1.4426950408889634f;
 #define AMSKV_ROWS_LAUNCH(DD, QB) \
     return launch<DD, QB, kHeld>(Q, O, enc, held, T, rows, kv_heads, group, max_keys, scale_log2, sm_count, stream)
+    // 16-row blocks of a CTA: one while all CTAs run at once (with codes, which every CTA widens for itself, only where that is little
+    // beside its latency), two likewise, else four.
+    // us per call with one / two / four: 16 items, T = 36, 64 keys: 64 channels 2.6 / 3.1 / 3.6, 128 channels 3.4 / 3.9 / 4.6, 8 bits
+    // 3.8 / 4.4 / 5.4 and 5.4 / 6.2 / 7.7;  32 items, T = 144, 484 keys: 6.7 / 8.2 / 10.0, 9.7 / 12.8 / 14.2, 8 bits 12.8 / 16.1 / 14.4 and
+    // 20.3 / 24.0 / 21.0;  64 items, T = 64, 1 024 keys: 8 bits 19.5 / 17.2 / 15.6;  64 items, T = 100, 256 keys: 6.5 / 5.7 / 6.4, 11.7 / 8.5 / 9.0,
+    // 8 bits 11.6 / 10.8 / 11.0 and 25.1 / 16.1 / 15.4;  128 items, T = 144, 256 keys: 11.8 / 11.1 / 12.3.
+    const int64_t blocks = (M + 15) / 16, items = (int64_t)rows * kv_heads;
+    const int64_t ones = kHeld && (D == 128 || max_keys > 512) ? sm_count : 2ll * sm_count;
+    const int qb = blocks == 1 || items * blocks <= ones ? 1 : blocks == 2 || (!kHeld && items * ((blocks + 1) / 2) <= 2ll * sm_count) ? 2 : 4;
     if (D == 64) {
-        if (M <= 16) AMSKV_ROWS_LAUNCH(64, 1);
-        if (M <= 32) AMSKV_ROWS_LAUNCH(64, 2);
+        if (qb == 1) AMSKV_ROWS_LAUNCH(64, 1);
+        if (qb == 2) AMSKV_ROWS_LAUNCH(64, 2);
         AMSKV_ROWS_LAUNCH(64, 4);
     }
-    if (M <= 16) AMSKV_ROWS_LAUNCH(128, 1);
-    if (M <= 32) AMSKV_ROWS_LAUNCH(128, 2);
+    if (qb == 1) AMSKV_ROWS_LAUNCH(128, 1);
+    if (qb == 2) AMSKV_ROWS_LAUNCH(128, 2);
     AMSKV_ROWS_LAUNCH(128, 4);
 #undef AMSKV_ROWS_LAUNCH
 }

@@ -63,7 +63,7 @@ struct TilesCfg {
     static constexpr uint32_t kQBytes = kQRows * D * 2, kQHalfBytes = kQRows * 128;
     static constexpr uint32_t kKVBytes = kKT * D * 2, kKVHalfBytes = kKT * 128;
     static constexpr uint32_t kStageBytes = 2 * kKVBytes;
-    static constexpr int kRing = kHeld ? 3 : 0;                 // tiles of codes on their way, each with 32 bytes behind it
+    static constexpr int kRing = kHeld ? 2 : 0;                 // tiles of codes on their way, each with 32 bytes behind it
     static constexpr uint32_t kCodeBytes = 2 * kKT * D, kRingBytes = kCodeBytes + 32;
     static constexpr uint32_t kSmemBytes = 2048 + 2 * kQBufs * kQBytes + kStages * kStageBytes + kRing * kRingBytes +
                                            (kHeld ? kHeldTab * 24 : 0);   // barriers and slack in front
@@ -74,7 +74,7 @@ struct TilesCfg {
 };
 
 struct Barriers {
-    uint64_t q_full[2][2], q_free[2][2], ring_full[3], ring_empty[3], kv_full[kMaxStages], kv_empty[kMaxStages], s_full[2][2], p_full[2][2], pv_done[2], o_full[2], drained[2];
+    uint64_t q_full[2][2], q_free[2][2], ring_full[2], ring_empty[2], kv_full[kMaxStages], kv_empty[kMaxStages], s_full[2][2], p_full[2][2], pv_done[2], o_full[2], drained[2];
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -383,6 +383,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             const int64_t values_at = (int64_t)held.capacity * D, scales_of_item = held.capacity / kBlock;
             uint32_t f_slot = 0, f_phase = 0, asked = 0;
             bool ended = false;
+            static_assert(C::kRing <= 2, "barriers");
             static_assert(C::kFetchWarps == 1 || C::kLoadWarps == 1, "one warp asks for codes");
             auto fetch = [&]() -> bool {   // the next tile into the ring
                 if (ended) return true;
