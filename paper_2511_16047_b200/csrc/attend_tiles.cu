@@ -6,19 +6,23 @@
 // have tiles of their own, which alternate.
 //   warps 0-3, 4-7   softmax of stream A, of stream B: a query row per thread (row = TMEM lane)
 //   then kMmaWarps   issue the products: one warp for both streams, or one for each
-//   then kLoadWarps  fill the ring of key/value stages
+//   then kLoadWarps  fill the stages of keys and values: with bulk copies, or by widening codes
+//   then kFetchWarps ask for codes (else the first loading warp does)
 // Per tile: S = Q K^T (128 x 64 fp32); the softmax warps exponentiate in base 2 against a reference maximum and write P as bf16 over S;
 // O += P V with P from tensor memory.  The reference is the maximum of the first tile; later tiles' maxima are not even taken: a row
 // whose sum over a tile leaves the range (beyond 2^64, or not a number) makes its warp take the true maxima, rescale O and the
 // sums, and form the tile again.
-//   64 channels: two CTAs per SM, so that 16 softmax warps keep the special-function unit busy.  One CTA of them, as below: 4 096
-//     queries x 10 521 keys x 64 heads 1 253 us, an 8-bit cache 1 682; two: T64C and T64H.
+//   64 channels: two CTAs per SM, so that 16 softmax warps keep the special-function unit busy.
 //   128 channels: one CTA per SM with two S buffers per stream (S of the next tile is formed while the softmax of this one runs), two
-//     issuing warps and two query tiles per stream, so that a unit's queries are there when it begins.
-// Why not the bulk copies of the paired kernel (attend_pair.cu): keys behind a row's last one may be anything, NaN among them, and
-// a product with a zero probability would spread it, so that the tail has to arrive as zeros, at an end that only the device
-// knows; and codes of 8 bits have to pass through registers to become bf16.  The loading warps use 16-byte asynchronous copies (zeros
-// where there is no key), or loads ahead of the tile that they widen.
+//     issuing warps and, over an encoder, two query tiles per stream, so that a unit's queries are there when it begins.
+// Keys behind a row's last one may be anything, NaN among them, and a product with a zero probability would spread it: the block
+// that a row's values do not fill comes in 16-byte asynchronous copies, with zeros behind the last key; all else in bulk copies.  Codes
+// come in bulk copies into a ring of tiles, from which warps widen them to bf16; where a tile's codes lie, and which of its slots
+// hold a key, is tabulated once per launch.
+// What bounds it: the exponentials, 64 channels (a tile's 8 192 take 512 cycles of an SM's special-function unit, the products 256), and
+// the products, 128 channels; with codes of 64 channels the issue slots that softmax and widening share.  4 096 queries x 10 521 keys x 64
+// heads: 64 channels 910 us (0.73 PFLOP/s of products), 128 channels 1 050 (1.26); from codes 1 040 to 1 270 and 1 250 (0.9 and 1.06).
+// 256 queries x 430 keys: 64 channels, 3 840 heads 179, codes 225; 128 channels, 2 048 heads 143, codes 175.
 // Every wait is bounded: one that gives up records a status code and sets a flag, its role stops, and so do the others at their
 // next wait.  Copies and products still under way are then awaited, and the tensor memory is freed.
 #include <algorithm>
@@ -919,7 +923,7 @@ cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, c
     if (oe != cudaSuccess) return oe;
     const int64_t slots = (int64_t)sm_count * C::kCtasPerSm, grid = std::min<int64_t>(plan.units, slots), rest = plan.units % slots;
     // Where SMs hold two CTAs and an eighth to two thirds of them have a unit in the last round, these must not share SMs: launched onto an
-    // idle chip they do not, onto SMs that come free one by one they do (UNEVEN).
+    // idle chip they do not, onto SMs that come free one by one they do.
     const bool uneven = C::kCtasPerSm == 2 && plan.units > slots && 8 * rest > slots && 3 * rest <= 2 * slots;
     return launch_kernel(!uneven, attend_tiles_kernel<D, kHeld>, dim3((unsigned)grid), dim3(C::kThreads), KernelMemory(C::kSmemBytes), stream, qm,
                          make_int3(pos[0], pos[1], pos[2]), om, make_int3(opos[0], opos[1], opos[2]), km, vm, vm16, make_int3(kpos[0], kpos[1], kpos[2]),

@@ -123,7 +123,7 @@ __device__ __forceinline__ void widen16_by(const uint4& codes, uint32_t word, bo
 {
     widen16(codes, scale_factor(word, values), scale_rest(word, values), lo, hi);
 }
-// 16 bytes global -> shared, zeros where !real (src must be readable-looking but is not read then)
+// 16 bytes global -> shared, zeros where !real (src is not read then)
 __device__ __forceinline__ void copy16_or_zero(uint32_t dst, const void* src, bool real)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");

@@ -192,3 +192,43 @@ def test_the_cache_is_left_alone_and_order_does_not_matter():
         torch.cuda.synchronize()
         _check(x, q, [(_np(k[r]), _np(v[r])) for r in range(rows)], 1, 0.125, "replayed")
         assert B.amskv_status(c.h) == 0
+
+
+@pytest.mark.parametrize("path", ["rows", "tiles"])
+@pytest.mark.parametrize("side", [2, 12])
+def test_offsets_beyond_32_bits(side, path):
+    """Rows of queries, outputs, keys and values 2^31 + 64 values apart."""
+    rows, heads, D, keys, apart = 3, 2, 64, 70, (1 << 31) + 64
+    T = side * side
+    base = torch.empty(2 * apart + 8 * heads * (keys + T) * D, dtype=torch.bfloat16, device="cuda")
+    one, two = heads * keys * D, heads * T * D
+    k, v = (torch.as_strided(base, (rows, heads, keys, D), (apart, keys * D, D, 1), n * one) for n in range(2))
+    q, o = (torch.as_strided(base, (rows, heads, T, D), (apart, T * D, D, 1), 2 * one + n * two) for n in range(2))
+    for x in (k, v, q):
+        x.copy_(torch.randn(x.shape, device="cuda"))
+    o.fill_(float("nan"))
+    with Cache(1, heads, D, rows, (side,), [(0, 1, False)]) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+        B.amskv_cross_attend(c.h, 0, heads, keys, k, v, q, o)
+        _check(o, q, [(_np(k[r]), _np(v[r])) for r in range(rows)], 1, 0.125, "far")
+        assert B.amskv_status(c.h) == 0
+
+
+def test_one_cache_on_two_streams():
+    """Cross attention reads nothing of the cache but its shapes, so that calls of one cache may overlap."""
+    rows, heads, D, keys, side = 4, 20, 128, 300, 12
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    q, k, v = ([torch.randn(rows, heads, n, D, device="cuda").bfloat16() for _ in range(2)] for n in (side * side, keys, keys))
+    outs = [[torch.empty_like(x) for x in q] for _ in range(4)]
+    with Cache(1, heads, D, rows, (side,), [(0, 1, False)]) as c:
+        torch.cuda.synchronize()
+        for j in range(2):
+            B.amskv_cross_attend(c.h, 0, heads, keys, k[j], v[j], q[j], outs[0][j])
+        torch.cuda.synchronize()
+        for out in outs[1:]:
+            for j in range(2):
+                B.amskv_cross_attend(c.h, 0, heads, keys, k[j], v[j], q[j], out[j], stream=streams[j])
+        torch.cuda.synchronize()
+        assert B.amskv_status(c.h) == 0
+    for out in outs[1:]:
+        assert torch.equal(out[0], outs[0][0]) and torch.equal(out[1], outs[0][1])

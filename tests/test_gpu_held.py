@@ -209,3 +209,89 @@ def test_a_layer_as_it_is_used(path):
                 w, size = ref.attention(_np(out[r]), _np(ek[r, :, :m]), _np(ev[r, :, :m]), 0.125)
                 assert (np.abs(_np(cross[r]) - w) <= 2.0 ** -8 * np.abs(w) + (2.0 ** -8 + 2.0 ** -9) * size).all()
             first += T
+
+
+@pytest.mark.parametrize("path", ["rows", "tiles"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_more_keys_than_the_tables_of_a_launch(D, path):
+    """12 544 keys, and more behind them with a short block between: tiles beyond the 192 that a launch tabulates."""
+    sides, rows, heads = (112, 3, 12, 2), 1, 3
+    steps = _steps(rows, heads, sides, D, D)
+    ks, vs = ([ref.held_values(_np(x[i])) for x in steps] for i in (1, 2))
+    with Cache(1, heads, D, rows, sides, [(0, 1, True)], flags=B.FLAG_KV_E4M3) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+        B.amskv_append(c.h, 0, 0, steps[0][1], steps[0][2])
+        for i in (1, 2, 3):
+            q, k, v = steps[i]
+            o = torch.full_like(q, float("nan"))
+            B.amskv_append_attend(c.h, 0, i, k, v, q, o)
+            assert B.amskv_status(c.h) == 0
+            _check(o, q, ks, vs, range(i + 1), 1.0 / math.sqrt(D), i)
+
+
+@pytest.mark.parametrize("path", ["rows", "tiles"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_blocks_of_large_values(D, path):
+    """Blocks whose power of two and bf16's least code exponent make more than one bf16 factor: |x| above 448 * 2^7."""
+    sides, rows, heads = (3, 4, 12), 2, 2
+    steps = _steps(rows, heads, sides, D, 3 * D)
+    for i, (q, k, v) in enumerate(steps):
+        q *= 2.0 ** -40
+        k *= 2.0 ** (40 if i != 1 else 0)      # blocks of both kinds in one tile
+        v[:, 0] *= 2.0 ** 60
+    ks, vs = ([ref.held_values(_np(x[i])) for x in steps] for i in (1, 2))
+    with Cache(1, heads, D, rows, sides, [(0, 1, True)], flags=B.FLAG_KV_E4M3) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+        for i, (q, k, v) in enumerate(steps):
+            o = torch.full_like(q, float("nan"))
+            B.amskv_append_attend(c.h, 0, i, k, v, q, o)
+            assert B.amskv_status(c.h) == 0
+            _check(o, q, ks, vs, range(i + 1), 1.0 / math.sqrt(D), i)
+
+
+@pytest.mark.parametrize("path", ["rows", "tiles"])
+def test_a_region_beyond_32_bits(path):
+    """More than 2^32 codes, and inputs of more than 2^31 values: the first items, some in the middle, the last."""
+    sides, rows, heads, D = (1, 2, 20), 2750, 16, 128
+    g = torch.Generator(device="cuda").manual_seed(7)
+    at = [0, 1373, 2749]
+    ks, vs = [], []
+    with Cache(1, heads, D, rows, sides, [(0, 1, True)], flags=B.FLAG_KV_E4M3) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+        assert B.amskv_cache_bytes(c.h)[0] > 1 << 32
+        for i, s in enumerate(sides):
+            q, k, v = (torch.randn(rows, heads, s * s, D, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+            o = torch.full_like(q, float("nan"))
+            B.amskv_append_attend(c.h, 0, i, k, v, q, o)
+            assert B.amskv_status(c.h) == 0
+            ks.append(ref.held_values(_np(k[at])))
+            vs.append(ref.held_values(_np(v[at])))
+            _check(o[at], q[at], ks, vs, range(i + 1), 1.0 / math.sqrt(D), i)
+            assert not torch.isnan(o.view(-1, D)[::4097]).any()
+        assert k.numel() > 1 << 31
+        B.amskv_read_segment(c.h, 0, 2, q, o)
+        assert (_np(q[at]) == ks[2]).all() and (_np(o[at]) == vs[2]).all()
+
+
+def test_two_caches_on_two_streams():
+    """Calls of two caches that overlap on the GPU give what they give one after the other."""
+    sides, rows, heads, D = (2, 5, 12, 16), 3, 20, 64
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    data = [_steps(rows, heads, sides, D, seed) for seed in (21, 22)]
+    outs = [[[torch.empty_like(q) for q, _, _ in d] for d in data] for _ in range(2)]
+    with Cache(1, heads, D, rows, sides, [(0, 1, True)], flags=B.FLAG_KV_E4M3) as a, Cache(1, heads, D, rows, sides, [(0, 1, True)], flags=B.FLAG_KV_E4M3) as b:
+        torch.cuda.synchronize()
+        for n in range(2):
+            for c in (a, b):
+                B.amskv_cache_reset(c.h)
+            for i in range(len(sides)):
+                for j, c in enumerate((a, b)):
+                    q, k, v = data[j][i]
+                    B.amskv_append_attend(c.h, 0, i, k, v, q, outs[n][j][i], streams[j])
+                    if n == 0:
+                        streams[j].synchronize()
+            torch.cuda.synchronize()
+        assert B.amskv_status(a.h) == 0 and B.amskv_status(b.h) == 0
+    for j in range(2):
+        for x, y in zip(outs[0][j], outs[1][j]):
+            assert torch.equal(x, y)
