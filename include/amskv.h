@@ -84,7 +84,7 @@ extern "C" {
                               named after the call, layer and scale (timeline tools show which kernels belong to
                               which step); no effect on results */
 
-#define AMSKV_FLAG_KV_E4M3 16u /* The cache holds K and V in 8 bits: e4m3 codes with a power of two for every block of 16 tokens of
+#define AMSKV_FLAG_KV_E4M3 32u /* The cache holds K and V in 8 bits: e4m3 codes with a power of two for every block of 16 tokens of
                               a (row, head) (K and V apart; the tokens of a scale, its last block possibly shorter), half the memory
                               and half the bytes that attention reads.  The power is the least 2^e, e >= -100, with no |x| of the
                               block above 448 * 2^e (1 for a block of zeros); a code is x * 2^-e rounded to nearest, ties to even;
@@ -499,7 +499,8 @@ AMSKV_API int amskv_rotary_table_bytes(const amskv_rotary_spec* spec, int64_t co
 
 /*
  * Fills a table: row n holds amplitude * (cos, sin) of the angles of position n, columns in axis-major order.  Made once for
- * a schedule (its scales one behind the other, say); angles are formed in fp64.
+ * a schedule (its scales one behind the other, say); angles are formed to 2^-32 of a turn, however far the position, and a position that
+ * is not a finite number gives entries that are not numbers.
  *   positions   device pointer to count * axes floats, 4-byte aligned
  *   table       device pointer, amskv_rotary_table_bytes() bytes, 16-byte aligned
  * Enqueued on `stream`.  Errors: INVALID, CUDA.

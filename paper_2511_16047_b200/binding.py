@@ -23,7 +23,7 @@ FLAG_PLAN_ONLY = 1
 FLAG_BULK_APPEND = 2
 FLAG_TRANSIENT_LAST_SCALE = 4
 FLAG_NVTX = 8
-FLAG_KV_E4M3 = 16
+FLAG_KV_E4M3 = 32
 PATH_AUTO, PATH_SIMT, PATH_TENSOR, PATH_TENSOR_PAIR, PATH_SMALL = 0, 1, 2, 3, 4
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BY_PARTS = 0, 1, 2, 3

@@ -2,7 +2,7 @@
 //
 // A block is 16 tokens of one (row, head); its power of two is the least 2^e with no |x| above 448 * 2^e (the largest e4m3), at
 // least 2^-100.  Powers of two cost a float code nothing but the headroom of one binade, and make code * 2^e exact in bf16, so that
-// attention over the cache is attention over bf16 values, and x * 2^-e exact in fp32, so that a value is rounded once.  Both are
+// attention over the cache is attention over bf16 values, and x * 2^-e exact too (or a zero in any case), so that a value is rounded once.  Both are
 // bound by memory: the append reads two bytes a channel and writes one.
 #include <cuda_fp8.h>
 

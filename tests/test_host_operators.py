@@ -97,7 +97,7 @@ def test_what_a_cache_of_8_bits_refuses():
         assert _code(B.amskv_cache_create, d) == B.ERR_UNSUPPORTED
     d, _k = B.make_desc(1, 2, 64, 2, (1, 2), [(0, 1, True)], flags=B.FLAG_KV_E4M3, token_budgets=[(5, 1)])
     assert _code(B.amskv_cache_required_bytes, d) == B.ERR_UNSUPPORTED
-    d, _k = B.make_desc(1, 2, 64, 2, (1, 2), [(0, 1, True)], flags=32)
+    d, _k = B.make_desc(1, 2, 64, 2, (1, 2), [(0, 1, True)], flags=16)
     assert _code(B.amskv_cache_required_bytes, d) == B.ERR_INVALID
     d, _k = B.make_desc(1, 2, 64, 2, (1, 2), [(0, 1, True)], flags=B.FLAG_KV_E4M3 | B.FLAG_PLAN_ONLY, token_budgets=[(0, 0)])
     c = B.amskv_cache_create(d)       # a budget of 0 is none
