@@ -273,10 +273,10 @@ void note_appended(amskv_cache* cache, int layer, int scale)
 // us per call, warp-matrix / tensor-memory, in a graph, 256 keys where nothing else is said:
 //   64 channels, an encoder:   T = 16  512 items 6.6 / 10.2, 8 192 88 / 99 (77 keys 67 / 60);  T = 36  128 6.3 / 8.9, 512 11.8 / 10.6;
 //     T = 100  128 8.2 / 9.0, 512 24.5 / 12.4;  T = 144  32 4.6 / 8.5, 128 11.1 / 8.7;  T = 256  32 5.7 / 9.0, 64 8.2 / 9.0
-//   64 channels, 8 bits:       T = 36  512 14.2 / 16.1, 2 048 53 / 56;  T = 64  2 048 60 / 62, 8 192 219 / 204;  T = 100  128 10.3 / 14.9, 512 29.8 / 17.2
+//   64 channels, 8 bits:       T = 36  512 14.2 / 16.1, 2 048 53 / 56;  T = 64  2 048 60 / 62, 8 192 219 / 204;  T = 100  64 10.4 / 22.3, 128 13.9 / 22.5, 256 20.0 / 22.6
 //   128 channels, an encoder:  T = 16  512 12.2 / 16.5, 8 192 184 / 205 (77 keys 127 / 111);  T = 64  128 9.3 / 9.6 (512 keys 15.0 / 13.5, 1 024 21.5 / 23.5),
 //     512 26.2 / 17.5;  T = 100  32 6.7 / 9.3, 64 8.5 / 9.3;  T = 144  16 5.1 / 8.2, 32 6.7 / 8.2, 64 11.5 / 8.5;  T = 256  16 6.7 / 8.9, 32 8.5 / 9.0
-//   128 channels, 8 bits:      T = 36  128 14.0 / 13.1, 512 30.4 / 23.8;  T = 100  32 13.3 / 15.4, 128 21.1 / 15.7;  T = 144  16 12.6 / 12.3, 32 14.8 / 12.5
+//   128 channels, 8 bits:      T = 36  128 11.3 / 13.1, 512 30.4 / 23.8;  T = 100  32 11.6 / 15.4, 64 13.6 / 15.4, 128 21.1 / 15.7;  T = 144  16 12.6 / 12.3, 32 14.8 / 12.5
 bool takes_tiles(const amskv_cache* cache, int32_t T, int32_t group, int64_t items, int64_t keys)
 {
     if (!cache->tc_ready || cache->path == AMSKV_PATH_SMALL || cache->path == AMSKV_PATH_SIMT) return false;

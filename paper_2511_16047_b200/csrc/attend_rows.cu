@@ -2,8 +2,8 @@
 // items, where a 128-row tile of the tensor-memory kernel (attend_tiles.cu) would be mostly empty.
 //
 // The query rows of a key/value head are those of all query heads that share it, one head behind the other: a few queries in each
-// of four heads fill one 16-row block and read the keys once.  A CTA of four warps takes kQB (1, 2, 4) such blocks and gives each
-// 4 / kQB warps, which share a chunk's 64 keys; a cluster of up to eight CTAs shares the keys of a call with few rows and many keys.
+// of four heads fill one 16-row block and read the keys once.  A CTA of four warps (eight) takes kQB (1, 2, 4) such blocks and gives each
+// kWarps / kQB warps, which share a chunk's 64 keys; a cluster of up to eight CTAs shares the keys of a call with few rows and many keys.
 // Every warp keeps its own reference maximum, sum and products; they are put together once at the end, through (distributed) shared
 // memory, without atomics, so that results are the same each time.
 //
@@ -19,12 +19,12 @@ namespace amskv {
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kChunk = 64;                 // keys of a stage
 constexpr float kRescaleLog2 = 8.f;        // a reference maximum moves when a chunk exceeds it by 2^8
 
-template <int D, bool kHeld>
+template <int D, bool kHeld, int kWarps>
 struct RowsCfg {
+    static constexpr int kThreads = kWarps * 32;
     static constexpr int kStages = kHeld ? 2 : 3;
     static constexpr int kRowBytes = D * 2;
     static constexpr int kTileBytes = kChunk * kRowBytes;
@@ -32,8 +32,8 @@ struct RowsCfg {
     static constexpr int kPartRow = D + 8;                                  // floats; shifts the banks of a row by 8
     static constexpr int kPartBytes = 16 * kPartRow * 4;                    // products of a warp's 16 rows
     static constexpr int kStatsAt = kWarps * kPartBytes;                    // maxima and sums of the rows behind them
-    static constexpr int kSmemBytes = kStages * kStageBytes;
-    static_assert(kStatsAt + 2 * kWarps * 16 * 8 <= kSmemBytes, "the parts take the place of the stages");
+    static constexpr int kPartsEnd = kStatsAt + 2 * kWarps * 16 * 8;        // the parts take the place of the stages
+    static constexpr int kSmemBytes = kStages * kStageBytes > kPartsEnd ? kStages * kStageBytes : kPartsEnd;
 };
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -68,20 +68,21 @@ __device__ __forceinline__ float2 ld_cluster_8B(uint32_t addr)
 }
 
 // Codes of one chunk on their way: a thread's 16-byte pieces of K and V, and the scale words of their blocks.
-template <int D>
+template <int D, int kThreads>
 struct HeldPieces {
     static constexpr int kPieces = D / 16, kRows = kThreads / kPieces, kN = kChunk / kRows;   // pieces of a row, rows of a pass, passes
     uint4 k[kN], v[kN];
     uint32_t scale[kN];
 };
 
-template <int D, int kQB, bool kHeld>
-__global__ void __launch_bounds__(kThreads, D == 64 ? 4 : 2)
+template <int D, int kQB, bool kHeld, int kWarps>
+__global__ void __launch_bounds__(kWarps * 32, (D == 64 ? 16 : 8) / kWarps)
 attend_rows_kernel(const __nv_bfloat16* Q, int64_t q_row, int64_t q_head, int64_t q_tok, __nv_bfloat16* O, int64_t o_row, int64_t o_head,
                    int64_t o_tok, const __grid_constant__ EncoderKeys enc, const __grid_constant__ HeldKeys held, int32_t T,
                    int32_t kv_heads, int32_t group, int32_t parts, int32_t splits, float scale_log2)
 {
-    using C = RowsCfg<D, kHeld>;
+    using C = RowsCfg<D, kHeld, kWarps>;
+    constexpr int kThreads = C::kThreads;
     constexpr int kKS = kWarps / kQB;                       // warps that share a chunk's keys
     constexpr int kWarpKeys = kChunk / kKS, kTiles = kWarpKeys / 8, kBlocks = kWarpKeys / kBlock;
     constexpr int kPieces = D / 32;                         // 16-byte pieces of a row per lane, in fragment order
@@ -137,7 +138,7 @@ attend_rows_kernel(const __nv_bfloat16* Q, int64_t q_row, int64_t q_head, int64_
         }
     };
     // ---- codes: fetch, then widen into a stage
-    using Pieces = HeldPieces<D>;
+    using Pieces = HeldPieces<D, kThreads>;
     Pieces next;
     const int w_piece = (int)threadIdx.x % Pieces::kPieces, w_row = (int)threadIdx.x / Pieces::kPieces;
     HeldView fetch = hv;
@@ -397,13 +398,13 @@ attend_rows_kernel(const __nv_bfloat16* Q, int64_t q_row, int64_t q_head, int64_
     ptx::cluster_sync();   // nobody's parts go while another reads them
 }
 
-template <int D, int kQB, bool kHeld>
+template <int D, int kQB, bool kHeld, int kWarps = 4>
 cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, const HeldKeys& held, int32_t T, int32_t rows,
                    int32_t kv_heads, int32_t group, int64_t max_keys, float scale_log2, int sm_count, cudaStream_t stream)
 {
-    using C = RowsCfg<D, kHeld>;
+    using C = RowsCfg<D, kHeld, kWarps>;
     static SharedMemoryOptIn opt_in;
-    const cudaError_t oe = opt_in.ensure(attend_rows_kernel<D, kQB, kHeld>, C::kSmemBytes);
+    const cudaError_t oe = opt_in.ensure(attend_rows_kernel<D, kQB, kHeld, kWarps>, C::kSmemBytes);
     if (oe != cudaSuccess) return oe;
     const int64_t blocks = ((int64_t)T * group + 15) / 16, parts = (blocks + kQB - 1) / kQB, ctas = parts * rows * kv_heads;
     // Few CTAs and several chunks of keys: clusters share them.  What a merge costs is about four chunks of an encoder's keys (in CTAs of
@@ -412,9 +413,15 @@ cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, c
     constexpr int kFirst = kHeld ? 4 : 8, kMore = kQB == 4 && !kHeld ? 8 : 4;
     const int64_t chunks = (max_keys + kChunk - 1) / kChunk;
     int32_t splits = 1;
-    while (splits < 8 && ctas * splits * 2 <= 2ll * sm_count && chunks >= (splits == 1 ? kFirst : splits * kMore)) splits *= 2;
+    const int64_t slots = kWarps == 8 && D == 128 ? sm_count : 2ll * sm_count;   // (a CTA of eight warps of 128 channels has an SM's registers)
+    while (splits < 8 && ctas * splits * 2 <= slots && chunks >= (splits == 1 ? kFirst : splits * kMore)) splits *= 2;
     if (ctas * splits > 0x7fffffffll) return cudaErrorInvalidValue;
-    return launch_kernel(true, attend_rows_kernel<D, kQB, kHeld>, dim3((unsigned)(ctas * splits)), dim3(kThreads),
+    // Behind an append, CTAs that are more than the SMs but do not fill them spread evenly over an idle chip, not over SMs that come free one
+    // by one: not overlapped with the launch before (64 channels: 128 items, T = 100 22 us, 19; 32 items, T = 400 43, 37).  An encoder's
+    // calls have no append before them and keep the 0.2 to 0.5 us of the overlap.
+    const int64_t grid = ctas * splits;
+    const bool uneven = kHeld && grid > sm_count && grid < (D == 64 ? 16 : 8) / kWarps * (int64_t)sm_count;
+    return launch_kernel(!uneven, attend_rows_kernel<D, kQB, kHeld, kWarps>, dim3((unsigned)grid), dim3(C::kThreads),
                          KernelMemory(C::kSmemBytes, (unsigned)splits), stream, (const __nv_bfloat16*)Q.ptr, Q.row, Q.head, Q.token,
                          (__nv_bfloat16*)O.ptr, O.row, O.head, O.token, enc, held, T, kv_heads, group, (int32_t)parts, splits, scale_log2);
 }
@@ -428,20 +435,28 @@ cudaError_t launch_any(const Strided& Q, const Strided& O, const EncoderKeys& en
     const float scale_log2 = softmax_scale * 1.4426950408889634f;
 #define AMSKV_ROWS_LAUNCH(DD, QB) \
     return launch<DD, QB, kHeld>(Q, O, enc, held, T, rows, kv_heads, group, max_keys, scale_log2, sm_count, stream)
-    // 16-row blocks of a CTA: one while all CTAs run at once (with codes, which every CTA widens for itself, only where that is little
-    // beside its latency), two likewise, else four.
-    // us per call with one / two / four: 16 items, T = 36, 64 keys: 64 channels 2.6 / 3.1 / 3.6, 128 channels 3.4 / 3.9 / 4.6, 8 bits
-    // 3.8 / 4.4 / 5.4 and 5.4 / 6.2 / 7.7;  32 items, T = 144, 484 keys: 6.7 / 8.2 / 10.0, 9.7 / 12.8 / 14.2, 8 bits 12.8 / 16.1 / 14.4 and
-    // 20.3 / 24.0 / 21.0;  64 items, T = 64, 1 024 keys: 8 bits 19.5 / 17.2 / 15.6;  64 items, T = 100, 256 keys: 6.5 / 5.7 / 6.4, 11.7 / 8.5 / 9.0,
-    // 8 bits 11.6 / 10.8 / 11.0 and 25.1 / 16.1 / 15.4;  128 items, T = 144, 256 keys: 11.8 / 11.1 / 12.3.
+    // 16-row blocks of a CTA: one while all CTAs run at once (with codes, which every CTA widens for itself, fewer of them the more keys
+    // there are), two likewise, else four.
+    // us per call with one / two / four: 16 items, T = 36, 64 keys: 64 channels 2.6 / 3.1 / 3.6, 128 channels 3.4 / 3.9 / 4.6;
+    // 32 items, T = 144, 484 keys: 6.7 / 8.2 / 10.0, 9.7 / 12.8 / 14.2;  64 items, T = 100, 256 keys: 6.5 / 5.7 / 6.4, 11.7 / 8.5 / 9.0;
+    // 128 items, T = 144, 256 keys: 11.8 / 11.1 / 12.3.
+    // 8 bits, with one / four blocks and eight warps: 16 items, T = 100, 164 keys 4.9 / 5.9 and 6.9 / 8.6, 584 keys 9.5 / 9.6 and 14.5 / 12.6;
+    // 32 items, T = 36, 520 keys 9.6 / 8.9 and 14.4 / 11.3, 1 060 keys 13.6 / 12.1 and 21.2 / 14.4.
     const int64_t blocks = (M + 15) / 16, items = (int64_t)rows * kv_heads;
-    const int64_t ones = kHeld && (D == 128 || max_keys > 512) ? sm_count : 2ll * sm_count;
+    const int64_t ones = !kHeld ? 2ll * sm_count : D == 64 ? (max_keys <= 512 ? 2ll : 1ll) * sm_count : max_keys <= 448 ? sm_count : sm_count / 2;
     const int qb = blocks == 1 || items * blocks <= ones ? 1 : blocks == 2 || (!kHeld && items * ((blocks + 1) / 2) <= 2ll * sm_count) ? 2 : 4;
+    // Codes: twice the warps, which widen them twice as fast, where all CTAs have an SM of their own (64 items, T = 100, 64 keys 7.2 us with
+    // four warps, 5.9 with eight, 128 channels 10.8, 8.7; 128 items, T = 64, 1 088 keys 21.5, 19.5, 128 channels, 484 keys 21.2, 18.7).
+    const bool eight = kHeld && qb == 4 && items * ((blocks + 3) / 4) <= sm_count;
     if (D == 64) {
+        if constexpr (kHeld)
+            if (eight) return launch<64, 4, kHeld, 8>(Q, O, enc, held, T, rows, kv_heads, group, max_keys, scale_log2, sm_count, stream);
         if (qb == 1) AMSKV_ROWS_LAUNCH(64, 1);
         if (qb == 2) AMSKV_ROWS_LAUNCH(64, 2);
         AMSKV_ROWS_LAUNCH(64, 4);
     }
+    if constexpr (kHeld)
+        if (eight) return launch<128, 4, kHeld, 8>(Q, O, enc, held, T, rows, kv_heads, group, max_keys, scale_log2, sm_count, stream);
     if (qb == 1) AMSKV_ROWS_LAUNCH(128, 1);
     if (qb == 2) AMSKV_ROWS_LAUNCH(128, 2);
     AMSKV_ROWS_LAUNCH(128, 4);
