@@ -14,10 +14,8 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 
-__device__ __forceinline__ uint32_t abs_max2(uint32_t a, uint32_t b)   // of two bf16 pairs without their signs, lane by lane
-{
-    return __vmaxu2(a & 0x7fff7fffu, b & 0x7fff7fffu);                 // (their bits are ordered as their values are)
-}
+__device__ __forceinline__ __nv_bfloat162 as_pair(uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); }
+__device__ __forceinline__ __nv_bfloat162 abs_max2(__nv_bfloat162 a, uint32_t b) { return __hmax2(a, __habs2(as_pair(b))); }   // (one instruction)
 // four bf16 pairs -> eight codes.  (The product with a power of two is exact, or so small that its code is a zero.)
 __device__ __forceinline__ uint2 codes_of(const uint4& x, __nv_bfloat162 inv)
 {
@@ -25,15 +23,15 @@ __device__ __forceinline__ uint2 codes_of(const uint4& x, __nv_bfloat162 inv)
     uint32_t c[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), inv);
+        const __nv_bfloat162 y = __hmul2(as_pair(w[i]), inv);
         const uint32_t bits = *reinterpret_cast<const uint32_t*>(&y);
         c[i] = __nv_cvt_float2_to_fp8x2(make_float2(__uint_as_float(bits << 16), __uint_as_float(bits & 0xffff0000u)), __NV_SATFINITE, __NV_E4M3);
     }
     return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
 }
 
-// A warp per block of K or of V.  Divisions by launch constants are multiplications: with the compiler's own, of 64 bits, they were a third of the
-// instructions (256 items, 1 024 tokens, 128 channels: 37.7 us, 29.3 now; 30.8 at the rate of a copy).
+// A warp per block of K or of V, which needs half the registers of one for both and leaves twice the warps to wait for memory (256 items,
+// 1 024 tokens, 128 channels: 37.7 us, 29.0; 30.8 at the rate of a copy).  Divisions by launch constants are multiplications.
 template <int D>
 __global__ void __launch_bounds__(kThreads)
 append_held_kernel(const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t k_row, int64_t k_head, int64_t k_tok, int64_t v_row,
@@ -53,9 +51,10 @@ append_held_kernel(const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t k_row
         uint4 x[kN];
 #pragma unroll
         for (int i = 0; i < kN; ++i) x[i] = i * (32 / kPieces) < left ? load_16B_once(src + i * (32 / kPieces) * tok_stride) : make_uint4(0, 0, 0, 0);
-        uint32_t top = 0;
+        __nv_bfloat162 most = as_pair(0);
 #pragma unroll
-        for (int i = 0; i < kN; ++i) top = abs_max2(abs_max2(abs_max2(top, x[i].x), abs_max2(x[i].y, x[i].z)), x[i].w);
+        for (int i = 0; i < kN; ++i) most = abs_max2(abs_max2(abs_max2(abs_max2(most, x[i].x), x[i].y), x[i].z), x[i].w);
+        const uint32_t top = *reinterpret_cast<const uint32_t*>(&most);   // (bits of numbers without a sign are ordered as the numbers are)
         const uint32_t amax = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));   // bits of a bf16
         // amax = (1 + f / 128) 2^(E - 127) <= 1.75 * 2^8 * 2^e
         const int32_t e = amax == 0 ? 0 : max((int32_t)(amax >> 7) - 135 + ((amax & 127u) > 96u ? 1 : 0), -100);
@@ -63,7 +62,7 @@ append_held_kernel(const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t k_row
         uint8_t* dst = codes + ((int64_t)item * 2 + kv) * ((int64_t)capacity * D) + (int64_t)(offset + b * kBlock) * D + lane * 8;
 #pragma unroll
         for (int i = 0; i < kN; ++i)
-            if (i * (32 / kPieces) < left) *reinterpret_cast<uint2*>(dst + i * 256) = codes_of(x[i], *reinterpret_cast<const __nv_bfloat162*>(&inv));
+            if (i * (32 / kPieces) < left) *reinterpret_cast<uint2*>(dst + i * 256) = codes_of(x[i], as_pair(inv));
         if (lane == 0) {
             const uint32_t word = scale_word(e, e);
             uint8_t* bytes = reinterpret_cast<uint8_t*>(scales + (int64_t)item * (capacity / kBlock) + offset / kBlock + b) + kv;

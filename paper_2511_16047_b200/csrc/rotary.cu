@@ -16,7 +16,7 @@ constexpr int kThreads = 256;
 // 10^6.  Here the frequency is a fraction of a turn in 64 bits, the position 24 bits and an exponent, and the 64 low bits of their product
 // lose whole turns by wrapping around, which is all the range reduction there is.  The top 32 bits of that, within an eighth of a turn
 // of a quarter, become an fp32 angle (off by 2^-23 of at most pi / 4) for the Taylor sums of sine (to the 9th power: 2e-9 is left) and
-// cosine (to the 10th: 1e-10).  What bounds it is the instructions: 131 071 x 64 entries 21.3 us, against 10.3 for the table's bytes;
+// cosine (to the 10th: 1e-10).  What bounds it is the instructions: 131 071 x 64 entries 22.0 us, against 10.3 for the table's bytes;
 // with fp64 angles 27.4, with 88-bit products and sincospif 31.2 (95 instructions an entry).
 struct TableRow {   // what a position is, for all its columns
     uint32_t m, sign;
