@@ -55,6 +55,11 @@ SHAPES = [
     (9, 3, 3, 64, 18, 333),        # 324 queries: three tiles
     (3, 3, 3, 128, 20, 65),
     (2, 2, 2, 128, 32, 1100),
+    # CTAs of two and of four 16-row blocks
+    (10, 4, 4, 64, 11, 200),
+    (8, 5, 5, 128, 11, 600),
+    (100, 3, 3, 64, 5, 150),
+    (100, 3, 3, 128, 9, 90),
     # several units per CTA: streams with tiles of their own, and (an odd number of them) one alone in a unit
     (40, 16, 16, 128, 2, 150),
     (110, 3, 3, 128, 2, 130),

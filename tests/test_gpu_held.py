@@ -64,6 +64,9 @@ def _check(out, q, ks, vs, kept, scale, what):
     (1, 2, 128, (20, 1, 4), (0, 1, True)),
     (110, 3, 128, (2, 7, 3), (0, 1, True)),            # several units per CTA, a stream alone in every other one
     (80, 9, 64, (3, 5), (0, 1, True)),
+    (4, 10, 64, (3, 12, 13), (0, 1, True)),            # an SM for each CTA of 64 query rows, with and without a share of the keys
+    (4, 5, 128, (3, 12, 13), (0, 1, True)),
+    (10, 12, 128, (3, 6, 8), (0, 1, True)),
 ])
 def test_a_schedule(rows, heads, D, sides, policy, path):
     steps = _steps(rows, heads, sides, D, sum(sides) + D)
