@@ -131,12 +131,16 @@ rotary_kernel(const __grid_constant__ RotaryArgs a, int32_t units)
 #pragma unroll
     for (int i = 0; i < 4; ++i) cs[i] = make_float4(1.f, 0.f, 1.f, 0.f);
     const int64_t n = a.index ? (int64_t)load_int(a.index + row * a.index_row + t) : a.first + t;
-    if (n >= 0 && n < a.table_rows) {   // (a token without a position keeps its channels)
+    if (n >= 0 && n < a.table_rows) {
         const float2* e = a.table + n * cols;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (i < 2 ? turn_first : turn_second)
                 cs[i] = load_float4(e + (i < 2 ? col_first : col_second) + 2 * (i & 1));
+    } else {
+        // A token without a position keeps its channels, bit for bit: turned by an angle of 0 an infinity would make its partner not a
+        // number, and a -0 would lose its sign.
+        turn_first = turn_second = false;
     }
     const int32_t head0 = blockIdx.y * kHeads;
     uint4 x[kHeads][2];

@@ -193,3 +193,22 @@ def test_captured_and_on_another_stream():
     graph.replay()
     torch.cuda.synchronize()
     _check(out, x, ref.rotary_angles(pos.cpu().numpy(), D, **kw), 2, False, 1.0, False, "replayed")
+
+
+@pytest.mark.parametrize("in_place", [False, True], ids=["out of place", "in place"])
+@pytest.mark.parametrize("interleaved", [False, True], ids=["half", "interleaved"])
+@pytest.mark.parametrize("rows,heads,T,D,dim", [(2, 3, 9, 64, 64), (37, 30, 36, 64, 48), (2, 2, 7, 128, 20)])
+def test_a_token_without_a_position_is_passed_on_bit_for_bit(rows, heads, T, D, dim, interleaved, in_place):
+    """Whatever its channels hold: infinities, numbers that are none, zeros with a sign."""
+    gen = torch.Generator(device="cuda").manual_seed(dim)
+    bits = torch.randint(-2 ** 15, 2 ** 15, (rows, heads, T, D), generator=gen, device="cuda", dtype=torch.int32).to(torch.int16)
+    bits[..., ::3], bits[..., 1::5], bits[..., 2::7] = 0x7f80, -0x8000, 0x7fc1      # infinity, -0, no number
+    spec, _ = _spec(dim, 1, interleaved, "plain")
+    table = _table(spec, dim, torch.arange(4, device="cuda").float()[:, None].contiguous())
+    index = torch.full((rows, T), -1, dtype=torch.int32, device="cuda")
+    index[:, ::2] = 4
+    for transposed in (False, True):
+        x = bits.clone().view(torch.bfloat16)
+        out = x if in_place else torch.zeros_like(x)
+        B.amskv_rotary(spec, table, 4, 0, index, rows, T, D, heads, x, out, transposed=transposed)
+        assert torch.equal(out.view(torch.int16), bits)
