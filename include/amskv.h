@@ -90,7 +90,8 @@ extern "C" {
                               block above 448 * 2^e (1 for a block of zeros); a code is x * 2^-e rounded to nearest, ties to even;
                               the value it stands for, code * 2^e, is exact in bf16, and attention is exact over these values
                               as it is over those of a bf16 cache.  A value comes back within 2^-4 of itself (half a step), or
-                              2^-10 * 2^e where it is below 2^-6 * 2^e.  |x| must be below 2^127.
+                              2^-10 * 2^e where it is below 2^-6 * 2^e.  |x| must be below 2^127, and for attention |V| times
+                              the number of keys below 2^104 (amskv_cross_attend).
                               Every scale starts on a block of its own, so that the arena rounds its room up to 16 tokens.
                               amskv_append_attend makes the two calls it stands for; the densities (amskv_attention_density,
                               amskv_attend_density) and AMSKV_PATH_SIMT are refused with UNSUPPORTED, and so are, at creation,
@@ -310,7 +311,9 @@ AMSKV_API int amskv_read_segment(amskv_cache* cache, int layer, int segment, voi
  *   kv_heads  divides heads: query head h reads key/value head h / (heads / kv_heads).
  *   Q, out    as for amskv_attend.  out must not overlap any input.  A row without keys gets zeros.
  * Path: AMSKV_PATH_SMALL and AMSKV_PATH_SIMT are the warp-matrix kernel, AMSKV_PATH_TENSOR and AMSKV_PATH_TENSOR_PAIR the tensor-memory
- * kernel.  Arithmetic as for amskv_attend.  Enqueued on `stream`.  Errors: INVALID, UNSUPPORTED (plan-only; keys above 2^30), CUDA.
+ * kernel.  Arithmetic as for amskv_attend; the sums of probabilities times values are formed in fp32 up to 2^24 times, or down to 2^-40 times,
+ * what they are in the end, so that |V| times the number of keys has to stay below 2^104, and outputs below 2^-60 lose digits.  Enqueued on
+ * `stream`.  Errors: INVALID, UNSUPPORTED (plan-only; keys above 2^30), CUDA.
  */
 typedef struct {
     int32_t kv_heads;

@@ -10,7 +10,7 @@
 //   then kFetchWarps ask for codes (else the first loading warp does)
 // Per tile: S = Q K^T (128 x 64 fp32); the softmax warps exponentiate in base 2 against a reference maximum and write P as bf16 over S;
 // O += P V with P from tensor memory.  The reference is the maximum of the first tile; later tiles' maxima are not even taken: a row
-// whose sum over a tile leaves the range (beyond 2^64, or not a number) makes its warp take the true maxima, rescale O and the
+// that outgrows it (by 2^64 in the sum over a tile, or to what is not a number) makes its warp take the true maxima, rescale O and the
 // sums, and form the tile again.
 //   64 channels: two CTAs per SM, so that 16 softmax warps keep the special-function unit busy.
 //   128 channels: one CTA per SM with two S buffers per stream (S of the next tile is formed while the softmax of this one runs), two
@@ -45,7 +45,11 @@ constexpr int kGroupWarps = 4;
 constexpr int kMmaWarp = 8;
 constexpr int kMaxStages = 4;
 constexpr float kRescaleLog2 = 8.f;
-constexpr float kSumLimit = 1.8446744e19f;   // 2^64
+// Probabilities are formed 2^kLowered below what the reference makes of them, so that a row may outgrow it by 2^64 while its sums stay below
+// 2^24: values are multiplied by no more, and fp32 holds their sums as long as (keys / 64) * |V| stays below 2^104.  (Formed as they
+// are, with a limit of 2^64, values of 2^64 were infinities in O; a limit of 2^14 instead costs 20 to 50 % where logits spread by 10.)
+constexpr float kLowered = 40.f;
+constexpr float kSumLimit = 16777216.f;      // 2^24
 constexpr int kHeldTab = 192;                // tiles of a cache that are tabulated in shared memory
 
 template <int D, bool kHeld>
@@ -703,7 +707,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                     };
                     if (j == 0) {
                         m_ref = tile_max();
-                        nb = -m_ref * scale_log2;
+                        nb = fmaf(-m_ref, scale_log2, -kLowered);
                     }
                     // P over S, bf16 (the type of V) for the product; the sums take the probabilities as they are.  Blocks behind the last one
                     // are not read by the product and keep stale bits.
@@ -751,10 +755,10 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                             tmem_wait_st();
                             const float mt = tile_max();
                             float alpha = 1.f;
-                            if (over || fmaf(mt, scale_log2, nb) > kRescaleLog2) {
+                            if (over || fmaf(mt, scale_log2, nb) > kRescaleLog2 - kLowered) {
                                 alpha = fast_exp2((m_ref - mt) * scale_log2);
                                 m_ref = mt;
-                                nb = -mt * scale_log2;
+                                nb = fmaf(-mt, scale_log2, -kLowered);
                                 l *= alpha;
                             }
 #pragma unroll 1

@@ -237,3 +237,24 @@ def test_one_cache_on_two_streams():
         assert B.amskv_status(c.h) == 0
     for out in outs[1:]:
         assert torch.equal(out[0], outs[0][0]) and torch.equal(out[1], outs[0][1])
+
+
+@pytest.mark.parametrize("path", sorted(PATHS))
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("growth", [0.0, 15.0, 40.0])
+@pytest.mark.parametrize("power", [100, -60])
+def test_large_and_small_values_behind_a_maximum_that_grows(power, growth, path, D):
+    """Logits near 0 in the first 64 keys and near `growth` behind: sums against the first keys' maximum have to stay in fp32 with
+    values near 2^100, and to be kept with values near 2^-60."""
+    rows, heads, side, keys = 2, 2, 12, 200
+    g = torch.Generator(device="cuda").manual_seed(D)
+    q = 0.1 * torch.randn(rows, heads, side * side, D, generator=g, device="cuda")
+    k, v = (torch.randn(rows, heads, keys, D, generator=g, device="cuda") for _ in range(2))
+    q[..., 0], k[..., 0], k[:, :, 64:, 0] = 1.0, 0.0, growth * math.sqrt(D)
+    q, k, v = (x.bfloat16() for x in (q, k, v * 2.0 ** power))
+    with Cache(1, heads, D, rows, (side,), [(0, 1, False)]) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+        out = torch.full_like(q, float("nan"))
+        B.amskv_cross_attend(c.h, 0, heads, keys, k, v, q, out)
+        assert B.amskv_status(c.h) == 0
+        _check(out, q, [(_np(k[r]), _np(v[r])) for r in range(rows)], 1, 1.0 / math.sqrt(D), "outgrown")

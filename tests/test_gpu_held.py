@@ -298,3 +298,25 @@ def test_two_caches_on_two_streams():
     for j in range(2):
         for x, y in zip(outs[0][j], outs[1][j]):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("path", sorted(PATHS))
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("growth", [0.0, 15.0, 40.0])
+@pytest.mark.parametrize("power", [88, -40])
+def test_large_and_small_values_behind_a_maximum_that_grows(power, growth, path, D):
+    """Logits near 0 in the first scale and near `growth` in the second."""
+    sides, rows, heads = (8, 12), 2, 2
+    steps = _steps(rows, heads, sides, D, 5 * D)
+    for i, (q, k, v) in enumerate(steps):
+        q *= 0.1
+        q[..., 0], k[..., 0] = 1.0, (growth * math.sqrt(D) if i else 0.0)
+        v *= 2.0 ** power
+    ks, vs = ([ref.held_values(_np(x[i])) for x in steps] for i in (1, 2))
+    with Cache(1, heads, D, rows, sides, [(0, 1, True)], flags=B.FLAG_KV_E4M3) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+        for i, (q, k, v) in enumerate(steps):
+            o = torch.full_like(q, float("nan"))
+            B.amskv_append_attend(c.h, 0, i, k, v, q, o)
+            assert B.amskv_status(c.h) == 0
+            _check(o, q, ks, vs, range(i + 1), 1.0 / math.sqrt(D), i)
