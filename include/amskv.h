@@ -312,8 +312,9 @@ AMSKV_API int amskv_read_segment(amskv_cache* cache, int layer, int segment, voi
  *   Q, out    as for amskv_attend.  out must not overlap any input.  A row without keys gets zeros.
  * Path: AMSKV_PATH_SMALL and AMSKV_PATH_SIMT are the warp-matrix kernel, AMSKV_PATH_TENSOR and AMSKV_PATH_TENSOR_PAIR the tensor-memory
  * kernel.  Arithmetic as for amskv_attend; the sums of probabilities times values are formed in fp32 up to 2^24 times, or down to 2^-40 times,
- * what they are in the end, so that |V| times the number of keys has to stay below 2^104, and outputs below 2^-60 lose digits.  Enqueued on
- * `stream`.  Errors: INVALID, UNSUPPORTED (plan-only; keys above 2^30), CUDA.
+ * what they are in the end, so that |V| times the number of keys has to stay below 2^104, and outputs below 2^-60 lose digits.  A NaN goes where the
+ * formula takes it: from a query to its outputs, from a key to those of all queries over it, from a value to its channel.  Enqueued on `stream`.
+ * Errors: INVALID, UNSUPPORTED (plan-only; keys above 2^30), CUDA.
  */
 typedef struct {
     int32_t kv_heads;

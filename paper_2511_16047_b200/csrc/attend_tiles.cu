@@ -723,7 +723,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                                     float x0, x1, p0, p1;
                                     fma2(x0, x1, __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]), scale_log2, scale_log2, nb, nb);
                                     if (C::kPolyEvery > 0 && i % (C::kPolyEvery > 0 ? C::kPolyEvery : 1) == 0) {
-                                        exp2_poly2(p0, p1, x0, x1);
+                                        exp2_poly2_nan(p0, p1, x0, x1);
                                     } else {
                                         p0 = fast_exp2(x0);
                                         p1 = fast_exp2(x1);

@@ -424,6 +424,25 @@ __device__ __forceinline__ void exp2_poly2(float& y0, float& y1, float x0, float
     y0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(r0) << 23));
     y1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(r1) << 23));
 }
+// The same for inputs that may be no number, which stay so: clamped by instructions that keep them, and 2^n a factor of its own.
+__device__ __forceinline__ void exp2_poly2_nan(float& y0, float& y1, float x0, float x1)
+{
+    constexpr float kMagic = 12582912.f;   // 1.5 * 2^23
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;\n"   // -127
+        "min.NaN.f32 %0, %0, 0f42FC0000;\n"   // 126
+        "max.NaN.f32 %1, %1, 0fC2FE0000;\n"
+        "min.NaN.f32 %1, %1, 0f42FC0000;\n"
+        : "+f"(x0), "+f"(x1));
+    float r0, r1, n0, n1, f0, f1, p0, p1;
+    add2(r0, r1, x0, x1, kMagic, kMagic);
+    add2(n0, n1, r0, r1, -kMagic, -kMagic);
+    fma2(f0, f1, n0, n1, -1.f, -1.f, x0, x1);
+    fma2(p0, p1, f0, f1, 0.0555041f, 0.0555041f, 0.2402265f, 0.2402265f);
+    fma2(p0, p1, p0, p1, f0, f1, 0.6931472f, 0.6931472f);
+    fma2(p0, p1, p0, p1, f0, f1, 1.f, 1.f);
+    y0 = p0 * __uint_as_float((__float_as_uint(r0) << 23) + 0x3f800000u);
+    y1 = p1 * __uint_as_float((__float_as_uint(r1) << 23) + 0x3f800000u);
+}
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float y;

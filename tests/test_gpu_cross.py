@@ -258,3 +258,37 @@ def test_large_and_small_values_behind_a_maximum_that_grows(power, growth, path,
         B.amskv_cross_attend(c.h, 0, heads, keys, k, v, q, out)
         assert B.amskv_status(c.h) == 0
         _check(out, q, [(_np(k[r]), _np(v[r])) for r in range(rows)], 1, 1.0 / math.sqrt(D), "outgrown")
+
+
+@pytest.mark.parametrize("path", sorted(PATHS))
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_number_that_is_none_is_not_lost(path, D):
+    """A NaN in a key makes every output of its (row, head) one, a NaN in a value that channel's, wherever the key lies in its tile;
+    no other output changes."""
+    rows, heads, kv, side, keys = 2, 4, 2, 12, 200
+    g = torch.Generator(device="cuda").manual_seed(D)
+    q = torch.randn(rows, heads, side * side, D, generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn(rows, kv, keys, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    n = torch.tensor([keys, 150], dtype=torch.int32, device="cuda")
+    with Cache(1, heads, D, rows, (side,), [(0, 1, False)]) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+
+        def run(kk, vv):
+            out = torch.zeros_like(q)
+            B.amskv_cross_attend(c.h, 0, kv, keys, kk, vv, q, out, lengths=n)
+            assert B.amskv_status(c.h) == 0
+            return out
+
+        plain = run(k, v)
+        assert torch.isfinite(plain).all()
+        for at in [*range(0, 28), 36, 48, 60, 63, 64, 76, 128, 149]:
+            kk, vv = k.clone(), v.clone()
+            kk[1, 0, at, 3] = float("nan")
+            out = run(kk, v)
+            assert torch.isnan(out[1, :2]).all(), at
+            assert torch.equal(out[0], plain[0]) and torch.equal(out[1, 2:], plain[1, 2:]), at
+            vv[0, 1, at, 7] = float("nan")
+            out = run(k, vv)
+            assert torch.isnan(out[0, 2:, :, 7]).all(), at
+            out[0, 2:, :, 7] = plain[0, 2:, :, 7]
+            assert torch.equal(out, plain), at
