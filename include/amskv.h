@@ -91,7 +91,8 @@ extern "C" {
                               the value it stands for, code * 2^e, is exact in bf16, and attention is exact over these values
                               as it is over those of a bf16 cache.  A value comes back within 2^-4 of itself (half a step), or
                               2^-10 * 2^e where it is below 2^-6 * 2^e.  |x| must be below 2^127, and for attention |V| times
-                              the number of keys below 2^104 (amskv_cross_attend).
+                              the number of keys below 2^104 (amskv_cross_attend).  A block with an infinity or a NaN is NaN in
+                              whole, for amskv_read_segment as for attention.
                               Every scale starts on a block of its own, so that the arena rounds its room up to 16 tokens.
                               amskv_append_attend makes the two calls it stands for; the densities (amskv_attention_density,
                               amskv_attend_density) and AMSKV_PATH_SIMT are refused with UNSUPPORTED, and so are, at creation,

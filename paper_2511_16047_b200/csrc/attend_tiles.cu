@@ -356,7 +356,8 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
         } else {
             // Codes land in a ring of their own by bulk copies of whole blocks, and with them the scale words of the
             // four blocks and the number of slots that the products read (0: there is no further tile).  Slots without a key keep what
-            // they held: any code is a finite number, and its probability is zero.  (Fetched into registers instead, a wait for a tile's codes
+            // they held: any code times a block's power is a finite number, and its probability is zero (but in a block that is no number, whose
+            // row is none either).  (Fetched into registers instead, a wait for a tile's codes
             // waits for all younger ones too, as loads are counted, not named; with 16-byte copies of every lane the copies took as
             // many instructions as the widening.)
             using Share = CodeShare<D>;

@@ -2,8 +2,9 @@
 //
 // A block is 16 tokens of one (row, head); its power of two is the least 2^e with no |x| above 448 * 2^e (the largest e4m3), at
 // least 2^-100.  Powers of two cost a float code nothing but the headroom of one binade, and make code * 2^e exact in bf16, so that
-// attention over the cache is attention over bf16 values, and x * 2^-e exact too (or a zero in any case), so that a value is rounded once.  Both are
-// bound by memory: the append reads two bytes a channel and writes one.
+// attention over the cache is attention over bf16 values, and x * 2^-e exact too (or a zero in any case), so that a value is rounded once.
+// A block with an infinity or what is no number gets codes of 0 and an infinite power, whose products are NaN: nothing that reads the cache
+// has to look for it.  Both are bound by memory: the append reads two bytes a channel and writes one.
 #include <cuda_fp8.h>
 
 #include "keys.cuh"
@@ -15,7 +16,7 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 __device__ __forceinline__ __nv_bfloat162 as_pair(uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); }
-__device__ __forceinline__ __nv_bfloat162 abs_max2(__nv_bfloat162 a, uint32_t b) { return __hmax2(a, __habs2(as_pair(b))); }   // (one instruction)
+__device__ __forceinline__ __nv_bfloat162 abs_max2(__nv_bfloat162 a, uint32_t b) { return __hmax2_nan(a, __habs2(as_pair(b))); }   // (one instruction; keeps a NaN)
 // four bf16 pairs -> eight codes.  (The product with a power of two is exact, or so small that its code is a zero.)
 __device__ __forceinline__ uint2 codes_of(const uint4& x, __nv_bfloat162 inv)
 {
@@ -56,15 +57,16 @@ append_held_kernel(const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t k_row
         for (int i = 0; i < kN; ++i) most = abs_max2(abs_max2(abs_max2(abs_max2(most, x[i].x), x[i].y), x[i].z), x[i].w);
         const uint32_t top = *reinterpret_cast<const uint32_t*>(&most);   // (bits of numbers without a sign are ordered as the numbers are)
         const uint32_t amax = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));   // bits of a bf16
+        const bool none = amax >= 0x7f80u;
         // amax = (1 + f / 128) 2^(E - 127) <= 1.75 * 2^8 * 2^e
         const int32_t e = amax == 0 ? 0 : max((int32_t)(amax >> 7) - 135 + ((amax & 127u) > 96u ? 1 : 0), -100);
         const uint32_t inv = (uint32_t)(127 - e) * 0x00800080u;
         uint8_t* dst = codes + ((int64_t)item * 2 + kv) * ((int64_t)capacity * D) + (int64_t)(offset + b * kBlock) * D + lane * 8;
 #pragma unroll
         for (int i = 0; i < kN; ++i)
-            if (i * (32 / kPieces) < left) *reinterpret_cast<uint2*>(dst + i * 256) = codes_of(x[i], as_pair(inv));
+            if (i * (32 / kPieces) < left) *reinterpret_cast<uint2*>(dst + i * 256) = none ? make_uint2(0, 0) : codes_of(x[i], as_pair(inv));
         if (lane == 0) {
-            const uint32_t word = scale_word(e, e);
+            const uint32_t word = none ? kNoNumber : scale_word(e, e);
             uint8_t* bytes = reinterpret_cast<uint8_t*>(scales + (int64_t)item * (capacity / kBlock) + offset / kBlock + b) + kv;
             bytes[0] = (uint8_t)word;
             bytes[2] = (uint8_t)(word >> 16);

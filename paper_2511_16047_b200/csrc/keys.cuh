@@ -100,6 +100,8 @@ __device__ __forceinline__ uint32_t scale_word(int32_t ke, int32_t ve)
 {
     return (uint32_t)(min(ke, 7) + 247) | (uint32_t)(min(ve, 7) + 247) << 8 | (uint32_t)max(ke - 7, 0) << 16 | (uint32_t)max(ve - 7, 0) << 24;
 }
+// The word of a block that is no number: infinite factors, and nothing left (codes of 0 go with it).
+constexpr uint32_t kNoNumber = 0x0000ffffu;
 // of a word, for keys or values: the factor twice, and what is left of e
 __device__ __forceinline__ uint32_t scale_factor(uint32_t word, bool values) { return ((values ? word >> 8 : word) & 0xffu) * 0x00800080u; }
 __device__ __forceinline__ uint32_t scale_rest(uint32_t word, bool values) { return (values ? word >> 24 : word >> 16) & 0xffu; }

@@ -320,3 +320,50 @@ def test_large_and_small_values_behind_a_maximum_that_grows(power, growth, path,
             B.amskv_append_attend(c.h, 0, i, k, v, q, o)
             assert B.amskv_status(c.h) == 0
             _check(o, q, ks, vs, range(i + 1), 1.0 / math.sqrt(D), i)
+
+
+@pytest.mark.parametrize("path", sorted(PATHS))
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")], ids=["nan", "inf", "-inf"])
+def test_a_block_with_a_number_that_is_none_or_an_infinity_is_no_number(bad, D, path):
+    """It comes back as NaN in whole, its (row, head) attends to NaN, and nothing else changes; a clean append behind a reset
+    leaves nothing of it."""
+    sides, rows, heads = (3, 6, 9), 2, 3
+    steps = _steps(rows, heads, sides, D, 31)
+    scale = 1.0 / math.sqrt(D)
+    ks, vs = ([ref.held_values(_np(x[i])) for x in steps] for i in (1, 2))
+    with Cache(1, heads, D, rows, sides, [(0, 1, True)], flags=B.FLAG_KV_E4M3) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+
+        def run(data):
+            outs = []
+            B.amskv_cache_reset(c.h)
+            for i, (q, k, v) in enumerate(data):
+                outs.append(torch.zeros_like(q))
+                B.amskv_append_attend(c.h, 0, i, k, v, q, outs[-1])
+            assert B.amskv_status(c.h) == 0
+            return outs
+
+        plain = run(steps)
+        for which in (1, 2):
+            for tok in (0, 15, 17, 35):
+                data = [[x.clone() for x in step] for step in steps]
+                data[1][which][1, 2, tok, 5] = bad
+                outs = run(data)
+                back = [torch.zeros_like(steps[1][1]) for _ in range(2)]
+                B.amskv_read_segment(c.h, 0, 1, *back)
+                for n, want in ((0, ks[1]), (1, vs[1])):
+                    want = torch.from_numpy(want).cuda().bfloat16()
+                    if n + 1 == which:
+                        want[1, 2, tok // 16 * 16:tok // 16 * 16 + 16] = float("nan")
+                    assert torch.equal(torch.isnan(back[n]), torch.isnan(want)), (which, tok, n)
+                    assert torch.equal(back[n].nan_to_num(), want.nan_to_num()), (which, tok, n)
+                assert torch.equal(outs[0], plain[0])
+                for i in (1, 2):
+                    assert torch.isnan(outs[i][1, 2]).all(), (which, tok, i)
+                    outs[i][1, 2] = plain[i][1, 2]
+                    assert torch.equal(outs[i], plain[i]), (which, tok, i)
+        for i, (q, _, _) in enumerate(steps):
+            out = run(steps)[i]
+            assert torch.equal(out, plain[i])
+            _check(out, q, ks, vs, range(i + 1), scale, i)
