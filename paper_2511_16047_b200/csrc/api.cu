@@ -507,7 +507,7 @@ int amskv_attend(amskv_cache* cache, int layer, int scale, const void* Q, void* 
                                     cache->sm_count, static_cast<cudaStream_t>(stream));
         if (e == cudaErrorNotSupported)   // (strides that no tensor map holds, too)
             e = launch_attend_rows(q, o, keys, T, cache->rows, cache->heads, cache->head_dim, cache->softmax_scale, cache->sm_count,
-                                   static_cast<cudaStream_t>(stream));
+                                   cache->path != AMSKV_PATH_AUTO, static_cast<cudaStream_t>(stream));
         if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
         return AMSKV_OK;
     }
@@ -843,7 +843,7 @@ int amskv_cross_attend(amskv_cache* cache, int scale, const amskv_encoder* enc, 
                                 cache->sm_count, static_cast<cudaStream_t>(stream));
     if (e == cudaErrorNotSupported)   // (strides that no tensor map holds, too)
         e = launch_attend_rows(q, o, keys, T, cache->rows, enc->kv_heads, group, cache->head_dim, cache->softmax_scale, cache->sm_count,
-                               static_cast<cudaStream_t>(stream));
+                               cache->path != AMSKV_PATH_AUTO, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) { (void)cudaGetLastError(); return AMSKV_ERR_CUDA; }
     return AMSKV_OK;
 }

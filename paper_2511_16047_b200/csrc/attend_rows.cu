@@ -400,7 +400,7 @@ attend_rows_kernel(const __nv_bfloat16* Q, int64_t q_row, int64_t q_head, int64_
 
 template <int D, int kQB, bool kHeld, int kWarps = 4>
 cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, const HeldKeys& held, int32_t T, int32_t rows,
-                   int32_t kv_heads, int32_t group, int64_t max_keys, float scale_log2, int sm_count, cudaStream_t stream)
+                   int32_t kv_heads, int32_t group, int64_t max_keys, float scale_log2, int sm_count, bool fixed_form, cudaStream_t stream)
 {
     using C = RowsCfg<D, kHeld, kWarps>;
     static SharedMemoryOptIn opt_in;
@@ -414,7 +414,7 @@ cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, c
     const int64_t chunks = (max_keys + kChunk - 1) / kChunk;
     int32_t splits = 1;
     const int64_t slots = kWarps == 8 && D == 128 ? sm_count : 2ll * sm_count;   // (a CTA of eight warps of 128 channels has an SM's registers)
-    while (splits < 8 && ctas * splits * 2 <= slots && chunks >= (splits == 1 ? kFirst : splits * kMore)) splits *= 2;
+    while (!fixed_form && splits < 8 && ctas * splits * 2 <= slots && chunks >= (splits == 1 ? kFirst : splits * kMore)) splits *= 2;
     if (ctas * splits > 0x7fffffffll) return cudaErrorInvalidValue;
     // Behind an append, CTAs that are more than the SMs but do not fill them spread evenly over an idle chip, not over SMs that come free one
     // by one: not overlapped with the launch before (64 channels: 128 items, T = 100 22 us, 19; 32 items, T = 400 43, 37).  An encoder's
@@ -428,13 +428,14 @@ cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, c
 
 template <bool kHeld>
 cudaError_t launch_any(const Strided& Q, const Strided& O, const EncoderKeys& enc, const HeldKeys& held, int32_t T, int32_t rows,
-                       int32_t kv_heads, int32_t group, int32_t D, int64_t max_keys, float softmax_scale, int sm_count, cudaStream_t stream)
+                       int32_t kv_heads, int32_t group, int32_t D, int64_t max_keys, float softmax_scale, int sm_count, bool fixed_form,
+                       cudaStream_t stream)
 {
     const int64_t M = (int64_t)T * group;
     if (T < 1 || M > 0x7fffffff - 128 || (int64_t)rows * kv_heads > 0x7fffffffll) return cudaErrorInvalidValue;
     const float scale_log2 = softmax_scale * 1.4426950408889634f;
 #define AMSKV_ROWS_LAUNCH(DD, QB) \
-    return launch<DD, QB, kHeld>(Q, O, enc, held, T, rows, kv_heads, group, max_keys, scale_log2, sm_count, stream)
+    return launch<DD, QB, kHeld>(Q, O, enc, held, T, rows, kv_heads, group, max_keys, scale_log2, sm_count, fixed_form, stream)
     // 16-row blocks of a CTA: one while all CTAs run at once (with codes, which every CTA widens for itself, fewer of them the more keys
     // there are), two likewise, else four.
     // us per call with one / two / four: 16 items, T = 36, 64 keys: 64 channels 2.6 / 3.1 / 3.6, 128 channels 3.4 / 3.9 / 4.6;
@@ -442,21 +443,22 @@ cudaError_t launch_any(const Strided& Q, const Strided& O, const EncoderKeys& en
     // 128 items, T = 144, 256 keys: 11.8 / 11.1 / 12.3.
     // 8 bits, with one / four blocks and eight warps: 16 items, T = 100, 164 keys 4.9 / 5.9 and 6.9 / 8.6, 584 keys 9.5 / 9.6 and 14.5 / 12.6;
     // 32 items, T = 36, 520 keys 9.6 / 8.9 and 14.4 / 11.3, 1 060 keys 13.6 / 12.1 and 21.2 / 14.4.
+    // A fixed form does without all that depends on the number of items, which decides in what order keys are summed up.
     const int64_t blocks = (M + 15) / 16, items = (int64_t)rows * kv_heads;
     const int64_t ones = !kHeld ? 2ll * sm_count : D == 64 ? (max_keys <= 512 ? 2ll : 1ll) * sm_count : max_keys <= 448 ? sm_count : sm_count / 2;
-    const int qb = blocks == 1 || items * blocks <= ones ? 1 : blocks == 2 || (!kHeld && items * ((blocks + 1) / 2) <= 2ll * sm_count) ? 2 : 4;
+    const int qb = blocks == 1 || (!fixed_form && items * blocks <= ones) ? 1 : blocks == 2 || (!kHeld && !fixed_form && items * ((blocks + 1) / 2) <= 2ll * sm_count) ? 2 : 4;
     // Codes: twice the warps, which widen them twice as fast, where all CTAs have an SM of their own (64 items, T = 100, 64 keys 7.2 us with
     // four warps, 5.9 with eight, 128 channels 10.8, 8.7; 128 items, T = 64, 1 088 keys 21.5, 19.5, 128 channels, 484 keys 21.2, 18.7).
-    const bool eight = kHeld && qb == 4 && items * ((blocks + 3) / 4) <= sm_count;
+    const bool eight = kHeld && !fixed_form && qb == 4 && items * ((blocks + 3) / 4) <= sm_count;
     if (D == 64) {
         if constexpr (kHeld)
-            if (eight) return launch<64, 4, kHeld, 8>(Q, O, enc, held, T, rows, kv_heads, group, max_keys, scale_log2, sm_count, stream);
+            if (eight) return launch<64, 4, kHeld, 8>(Q, O, enc, held, T, rows, kv_heads, group, max_keys, scale_log2, sm_count, fixed_form, stream);
         if (qb == 1) AMSKV_ROWS_LAUNCH(64, 1);
         if (qb == 2) AMSKV_ROWS_LAUNCH(64, 2);
         AMSKV_ROWS_LAUNCH(64, 4);
     }
     if constexpr (kHeld)
-        if (eight) return launch<128, 4, kHeld, 8>(Q, O, enc, held, T, rows, kv_heads, group, max_keys, scale_log2, sm_count, stream);
+        if (eight) return launch<128, 4, kHeld, 8>(Q, O, enc, held, T, rows, kv_heads, group, max_keys, scale_log2, sm_count, fixed_form, stream);
     if (qb == 1) AMSKV_ROWS_LAUNCH(128, 1);
     if (qb == 2) AMSKV_ROWS_LAUNCH(128, 2);
     AMSKV_ROWS_LAUNCH(128, 4);
@@ -466,20 +468,21 @@ cudaError_t launch_any(const Strided& Q, const Strided& O, const EncoderKeys& en
 }  // namespace
 
 cudaError_t launch_attend_rows(const Strided& Q, const Strided& O, const EncoderKeys& enc, int32_t T, int32_t rows, int32_t kv_heads,
-                               int32_t group, int32_t D, float softmax_scale, int sm_count, cudaStream_t stream)
+                               int32_t group, int32_t D, float softmax_scale, int sm_count, bool fixed_form, cudaStream_t stream)
 {
     HeldKeys none;
     memset(&none, 0, sizeof(none));
-    return launch_any<false>(Q, O, enc, none, T, rows, kv_heads, group, D, enc.max_keys, softmax_scale, sm_count, stream);
+    return launch_any<false>(Q, O, enc, none, T, rows, kv_heads, group, D, enc.max_keys, softmax_scale, sm_count, fixed_form, stream);
 }
 
 cudaError_t launch_attend_rows(const Strided& Q, const Strided& O, const HeldKeys& held, int32_t T, int32_t rows, int32_t heads,
-                               int32_t D, float softmax_scale, int sm_count, cudaStream_t stream)
+                               int32_t D, float softmax_scale, int sm_count, bool fixed_form, cudaStream_t stream)
 {
     EncoderKeys none;
     memset(&none, 0, sizeof(none));
     if (held.ranges.n < 1 || held.blocks < 1) return cudaErrorInvalidValue;
-    return launch_any<true>(Q, O, none, held, T, rows, heads, 1, D, (int64_t)held.blocks * kBlock, softmax_scale, sm_count, stream);
+    return launch_any<true>(Q, O, none, held, T, rows, heads, 1, D, (int64_t)held.blocks * kBlock, softmax_scale, sm_count, fixed_form,
+                            stream);
 }
 
 }  // namespace amskv

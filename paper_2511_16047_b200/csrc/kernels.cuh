@@ -202,11 +202,12 @@ cudaError_t launch_append_held(const Strided& K, const Strided& V, const HeldReg
 // Positions offset .. offset + T - 1 of a layer's region (of bf16 values: scales null) to [rows, heads, T, D] tensors; K's strides hold for V.
 cudaError_t launch_read_segment(const void* region, const uint32_t* scales, int32_t capacity, int32_t offset, int32_t T, int32_t rows,
                                 int32_t heads, int32_t D, const Strided& K, const Strided& V, int sm_count, cudaStream_t stream);
-// Warp-matrix kernel over either (attend_rows.cu); `group` query heads share a key/value head.
+// Warp-matrix kernel over either (attend_rows.cu); `group` query heads share a key/value head.  fixed_form: the form is chosen by the shapes
+// of a row alone, so that its result does not depend on the number of rows and heads.
 cudaError_t launch_attend_rows(const Strided& Q, const Strided& O, const EncoderKeys& enc, int32_t T, int32_t rows, int32_t kv_heads,
-                               int32_t group, int32_t D, float softmax_scale, int sm_count, cudaStream_t stream);
+                               int32_t group, int32_t D, float softmax_scale, int sm_count, bool fixed_form, cudaStream_t stream);
 cudaError_t launch_attend_rows(const Strided& Q, const Strided& O, const HeldKeys& held, int32_t T, int32_t rows, int32_t heads,
-                               int32_t D, float softmax_scale, int sm_count, cudaStream_t stream);
+                               int32_t D, float softmax_scale, int sm_count, bool fixed_form, cudaStream_t stream);
 
 // Tensor-memory kernel over either (attend_tiles.cu).
 cudaError_t launch_attend_tiles(const Strided& Q, const Strided& O, const EncoderKeys& enc, int32_t T, int32_t rows, int32_t kv_heads,

@@ -292,3 +292,30 @@ def test_a_number_that_is_none_is_not_lost(path, D):
             assert torch.isnan(out[0, 2:, :, 7]).all(), at
             out[0, 2:, :, 7] = plain[0, 2:, :, 7]
             assert torch.equal(out, plain), at
+
+
+@pytest.mark.parametrize("path", ["rows", "tiles"])
+@pytest.mark.parametrize("D,kv,side,keys", [(64, 4, 1, 600), (64, 2, 3, 1100), (64, 4, 10, 130), (128, 4, 4, 600), (128, 1, 12, 200)])
+def test_a_path_of_ones_own_choice_depends_on_the_shapes_alone(D, kv, side, keys, path):
+    """Under every path but AUTO an image has the same outputs whatever other images it is computed with, bit for bit."""
+    heads, most = 4, 90
+    g = torch.Generator(device="cuda").manual_seed(D + keys)
+    q = torch.randn(most, heads, side * side, D, generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn(most, kv, keys, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    n = torch.tensor(_lengths(most, keys), dtype=torch.int32, device="cuda")
+    want = None
+    for rows in (most, 1, 2, 9, 30):
+        with Cache(1, heads, D, rows, (side,), [(0, 1, False)]) as c:
+            B.amskv_set_attend_path(c.h, PATHS[path])
+            out = torch.zeros_like(q[:rows])
+            B.amskv_cross_attend(c.h, 0, kv, keys, k[:rows], v[:rows], q[:rows], out, lengths=n[:rows])
+            assert B.amskv_status(c.h) == 0
+        want = out if want is None else want
+        assert torch.equal(out, want[:rows]), rows
+
+
+@pytest.mark.parametrize("shape", [(3, 1, 1, 64, 20, 512), (2, 4, 2, 64, 2, 700), (2, 4, 2, 64, 2, 1300), (3, 2, 2, 64, 15, 520),
+                                   (2, 4, 2, 128, 2, 700), (2, 4, 2, 128, 2, 1300), (3, 2, 1, 128, 7, 520)], ids=lambda s: "x".join(map(str, s)))
+def test_clusters_that_share_long_keys(shape):
+    """Two, four and eight CTAs to a row's keys, which only calls of few items under AUTO have."""
+    test_rows_of_different_lengths(shape, "auto")

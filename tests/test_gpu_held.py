@@ -367,3 +367,40 @@ def test_a_block_with_a_number_that_is_none_or_an_infinity_is_no_number(bad, D, 
             out = run(steps)[i]
             assert torch.equal(out, plain[i])
             _check(out, q, ks, vs, range(i + 1), scale, i)
+
+
+@pytest.mark.parametrize("path", ["rows", "tiles"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_path_of_ones_own_choice_depends_on_the_scale_alone(D, path):
+    """Under every path but AUTO an image has the same outputs whatever other images it is computed with, bit for bit."""
+    sides, heads = (1, 2, 4, 6, 10, 16), 5
+    steps = _steps(60, heads, sides, D, 17)
+    want = None
+    for rows in (60, 2, 8, 30):
+        with Cache(1, heads, D, rows, sides, [(0, 1, True)], flags=B.FLAG_KV_E4M3) as c:
+            B.amskv_set_attend_path(c.h, PATHS[path])
+            outs = []
+            for i, step in enumerate(steps):
+                q, k, v = (x[:rows].contiguous() for x in step)
+                outs.append(torch.zeros_like(q))
+                B.amskv_append_attend(c.h, 0, i, k, v, q, outs[-1])
+            assert B.amskv_status(c.h) == 0
+        want = want or outs
+        for i, (a, b) in enumerate(zip(outs, want)):
+            assert torch.equal(a, b[:rows]), (rows, i)
+
+
+@pytest.mark.parametrize("rows,heads,D,sides", [
+    (2, 1, 64, (32, 2)),       # eight CTAs to the keys
+    (16, 5, 64, (24, 5)),      # CTAs of two blocks, two to the keys
+    (1, 5, 64, (5, 24)),       # eight warps, four CTAs to the keys
+    (1, 1, 128, (22, 2)),
+    (2, 1, 128, (32, 2)),
+    (16, 5, 128, (13, 5)),     # two blocks, alone and two CTAs to the keys
+    (8, 5, 128, (22, 5)),      # and four
+    (4, 5, 128, (21, 9)),      # eight warps, two
+    (2, 5, 128, (20, 11)),     # and four
+])
+def test_clusters_that_share_long_keys(rows, heads, D, sides):
+    """Forms that only calls of few items under AUTO have."""
+    test_a_schedule(rows, heads, D, sides, (0, 1, True), "auto")
