@@ -152,6 +152,27 @@ def _int32(name: str, x) -> None:
         raise OverflowError("%s out of range" % name)
 
 
+def _int64(name: str, x) -> int:
+    """ctypes would take the low 64 bits of a longer int."""
+    if not -2 ** 63 <= int(x) < 2 ** 63:
+        raise OverflowError("%s out of range" % name)
+    return int(x)
+
+
+def _list(name: str, x, dtype: str, count: int) -> Optional[int]:
+    """Address of a device list of at least `count` numbers, contiguous (what is given as an address is the caller's to know)."""
+    if hasattr(x, "data_ptr"):
+        _is_of(name, x, dtype)
+        if not x.is_contiguous() or x.numel() < count:
+            raise ValueError("%s: expected %d contiguous numbers, not %s with strides %s" % (name, count, tuple(x.shape), tuple(x.stride())))
+    return _addr(x)
+
+
+def _is_of(name: str, x, dtype: str) -> None:
+    if str(x.dtype) != "torch." + dtype:
+        raise ValueError("%s: expected %s, not %s" % (name, dtype, x.dtype))
+
+
 def _addr(x) -> Optional[int]:
     if x is None:
         return None
@@ -287,7 +308,8 @@ def amskv_read_segment(cache: int, layer: int, segment: int, K, V, stream=None) 
 def amskv_cross_attend(cache: int, scale: int, kv_heads: int, keys: int, K, V, Q, out, lengths=None, offsets=None, max_keys: int = 0,
                        stream=None) -> None:
     """The queries of `scale` over an encoder's states: K and V [rows, kv_heads, keys, D] with device int32 `lengths` [rows], or,
-    with device int32 `offsets` [rows + 1], [1, kv_heads, keys, D] (all rows one behind the other)."""
+    with device int32 `offsets` [rows + 1], [1, kv_heads, keys, D] (all rows one behind the other).  Lists of another type or of fewer
+    numbers (than Q has rows, where it is a tensor) raise ValueError."""
     if _steps is not None:
         rc = _steps.cross_attend(cache, scale, kv_heads, keys, K, V, Q, out, lengths, offsets, max_keys, stream)
         if rc is not None:
@@ -295,7 +317,8 @@ def amskv_cross_attend(cache: int, scale: int, kv_heads: int, keys: int, K, V, Q
     for name, x in (("scale", scale), ("kv_heads", kv_heads), ("keys", keys), ("max_keys", max_keys)):
         _int32(name, x)
     assert all(not hasattr(x, "is_contiguous") or x.is_contiguous() for x in (lengths, offsets)), "expected contiguous lists"
-    enc = Encoder(kv_heads, keys, max_keys, _addr(lengths), _addr(offsets))
+    rows = Q.shape[0] if hasattr(Q, "shape") and len(Q.shape) == 4 else 0
+    enc = Encoder(kv_heads, keys, max_keys, _list("lengths", lengths, "int32", rows), _list("offsets", offsets, "int32", rows + 1 if rows else 0))
     _check(lib.amskv_cross_attend(cache, scale, ctypes.byref(enc), _addr(K), _addr(V), _kv_strides(K, V), _addr(Q), _addr(out), _strides(Q),
                                   _strides(out), _stream(stream)), "amskv_cross_attend")
 
@@ -351,28 +374,43 @@ def amskv_rotary_table_bytes(spec: RotarySpec, count: int) -> int:
 
 
 def amskv_rotary_table(spec: RotarySpec, positions, count: int, table, stream=None) -> None:
-    """positions: device floats [count, axes]; table: device floats [count, rotary_dim / 2, 2]."""
-    _check(lib.amskv_rotary_table(ctypes.byref(spec), _addr(positions), int(count), _addr(table), _stream(stream)),
-           "amskv_rotary_table")
+    """positions: device floats [count, axes]; table: device floats [count, rotary_dim / 2, 2].  Tensors of another type, with gaps, or
+    of fewer numbers raise ValueError."""
+    count = _int64("count", count)
+    _check(lib.amskv_rotary_table(ctypes.byref(spec), _list("positions", positions, "float32", count * spec.axes), count,
+                                  _list("table", table, "float32", count * spec.rotary_dim), _stream(stream)), "amskv_rotary_table")
 
 
 def amskv_rotary(spec: RotarySpec, table, table_rows: int, first: int, index, rows: int, T: int, head_dim: int, q_heads: int, Q,
                  Q_out, k_heads: int = 0, K=None, K_out=None, transposed: bool = False, stream=None, index_row_stride=None) -> None:
     """Rotates Q (and K) by rows first .. first + T - 1 of the table, or by the rows `index` names: device int32 [T] or
-    [rows, T] (a tensor, or an address with index_row_stride)."""
+    [rows, T] (a tensor, or an address with index_row_stride).  A table or an index of another type or of fewer numbers, a table
+    with gaps: ValueError."""
     if _steps is not None:
         rc = _steps.rotary(spec, table, table_rows, first, index, index_row_stride, rows, T, head_dim, q_heads, Q, Q_out, k_heads, K, K_out,
                            transposed, stream)
         if rc is not None:
             return _check(rc, "amskv_rotary")
-    if index_row_stride is None:
+    given = index_row_stride
+    if given is None:
         index_row_stride = 0
-        if hasattr(index, "stride"):
-            assert index.dim() in (1, 2) and (index.shape[-1] == 1 or index.stride(-1) == 1), "expected [T] or [rows, T], tokens contiguous"
-            index_row_stride = index.stride(0) if index.dim() == 2 else 0
     for name, x in (("rows", rows), ("T", T), ("head_dim", head_dim), ("q_heads", q_heads), ("k_heads", k_heads)):
         _int32(name, x)
-    _check(lib.amskv_rotary(ctypes.byref(spec), _addr(table), int(table_rows), int(first), _addr(index), int(index_row_stride), rows, T,
+    if hasattr(index, "stride"):
+        assert index.dim() in (1, 2) and (index.shape[-1] == 1 or index.stride(-1) == 1), "expected [T] or [rows, T], tokens contiguous"
+        _is_of("index", index, "int32")
+        if given is None:
+            index_row_stride = index.stride(0) if index.dim() == 2 else 0
+            short = index.shape[-1] < T or (index.dim() == 2 and index.shape[0] < rows)
+        else:
+            last = sum((n - 1) * s for n, s in zip(index.shape, index.stride())) if index.numel() else -1
+            short = (rows - 1) * int(given) + T - 1 > last
+        if short:
+            raise ValueError("index: %s with strides %s is too short for %d rows of %d tokens" % (tuple(index.shape), tuple(index.stride()), rows, T))
+    for name, x in (("table_rows", table_rows), ("first", first), ("index_row_stride", index_row_stride)):
+        _int64(name, x)
+    _check(lib.amskv_rotary(ctypes.byref(spec), _list("table", table, "float32", int(table_rows) * spec.rotary_dim), int(table_rows), int(first),
+                            _addr(index), int(index_row_stride), rows, T,
                             head_dim, q_heads, _addr(Q), _strides(Q), _addr(Q_out), _strides(Q_out), k_heads, _addr(K), _strides(K),
                             _addr(K_out), _strides(K_out), ROTARY_TRANSPOSED if transposed else 0, _stream(stream)), "amskv_rotary")
 

@@ -29,7 +29,8 @@ typedef int (*append_attend_fn)(void*, int, int, const void*, const void*, const
 static append_fn f_append;
 static attend_fn f_attend;
 static append_attend_fn f_append_attend;
-static PyObject *s_data_ptr, *s_is_contiguous, *s_stride, *s_cuda_stream;
+static PyObject *s_data_ptr, *s_is_contiguous, *s_stride, *s_cuda_stream, *s_dtype, *s_numel, *s_shape, *s_torch;
+static PyObject *torch_int32, *torch_float32; /* looked up when a tensor is first checked for them */
 
 /* The helpers below return 0, or -1 for an argument that is left to ctypes (with or without an error set). */
 
@@ -87,12 +88,58 @@ static int as_int64(PyObject* o, int64_t* out)
     return PyErr_Occurred() ? -1 : 0;
 }
 
+/* whether a tensor's elements are of the type `name` of torch */
+static int is_of(PyObject* x, PyObject** type, const char* name)
+{
+    if (!*type) {
+        PyObject* torch = PyImport_GetModule(s_torch);
+        if (!torch) return -1;
+        *type = PyObject_GetAttrString(torch, name);
+        Py_DECREF(torch);
+        if (!*type) return -1;
+    }
+    PyObject* d = PyObject_GetAttr(x, s_dtype);
+    if (!d) return -1;
+    const int same = d == *type;
+    Py_DECREF(d);
+    return same ? 0 : -1;
+}
+
+/* address of a contiguous list of at least `count` numbers of a type: None, an int or a tensor */
+static int list_of(PyObject* x, PyObject** type, const char* name, int64_t count, void** out)
+{
+    int64_t s[3], n = 0;
+    int strided;
+    if (tensor(x, out, s, &strided) || strided) return -1;
+    if (x == Py_None || PyLong_CheckExact(x)) return 0;
+    if (is_of(x, type, name)) return -1;
+    PyObject* r = PyObject_CallMethodNoArgs(x, s_numel);
+    if (!r) return -1;
+    const int bad = as_int64(r, &n);
+    Py_DECREF(r);
+    return bad || n < count ? -1 : 0;
+}
+
+/* extents of a tensor into shape[most]; the number of dimensions, or -1 */
+static int shape_of(PyObject* x, int64_t* shape, int most)
+{
+    PyObject* r = PyObject_GetAttr(x, s_shape);
+    if (!r) return -1;
+    int n = PyTuple_Check(r) && PyTuple_GET_SIZE(r) <= most ? (int)PyTuple_GET_SIZE(r) : -1;
+    for (int i = 0; i < n; ++i)
+        if (as_int64(PyTuple_GET_ITEM(r, i), &shape[i])) n = -1;
+    Py_DECREF(r);
+    return n;
+}
+
 /* address of a list of table rows, and the stride of its rows: None, an int with `given`, or a tensor [T] or [rows, T] */
-static int index_of(PyObject* x, PyObject* given, void** addr, int64_t* row_stride)
+static int index_of(PyObject* x, PyObject* given, int rows, int T, void** addr, int64_t* row_stride)
 {
     *row_stride = 0;
     if (given != Py_None && as_int64(given, row_stride)) return -1;
     if (x == Py_None || PyLong_CheckExact(x)) return as_pointer(x, addr);
+    int64_t shape[2];
+    if (is_of(x, &torch_int32, "int32") || shape_of(x, shape, 2) < 1) return -1;
     PyObject* r = PyObject_CallMethodNoArgs(x, s_data_ptr);
     if (!r) return -1;
     const int bad = as_pointer(r, addr);
@@ -104,8 +151,13 @@ static int index_of(PyObject* x, PyObject* given, void** addr, int64_t* row_stri
     int64_t last = 0, first = 0;
     int ok = (n == 1 || n == 2) && !as_int64(PyTuple_GET_ITEM(r, n - 1), &last) && last == 1 && !as_int64(PyTuple_GET_ITEM(r, 0), &first);
     Py_DECREF(r);
-    if (given == Py_None) *row_stride = n == 2 ? first : 0;
-    return ok ? 0 : -1;
+    if (!ok) return -1;
+    if (given == Py_None) {
+        *row_stride = n == 2 ? first : 0;
+        return shape[n - 1] >= T && (n == 1 || shape[0] >= rows) ? 0 : -1;
+    }
+    const __int128 there = shape[0] < 1 || shape[n - 1] < 1 ? 0 : (n == 2 ? (__int128)(shape[0] - 1) * first : 0) + shape[n - 1];
+    return (__int128)(rows - 1) * *row_stride + T <= there ? 0 : -1;
 }
 
 static int stream_of(PyObject* s, void** out) /* None, an address, or something with .cuda_stream */
@@ -195,6 +247,13 @@ static PyObject* py_append_attend(PyObject* self, PyObject* const* args, Py_ssiz
     return PyLong_FromLong(rc);
 }
 
+/* floats in `rows` rows of a table (arguments that make no sense are the library's to refuse) */
+static int64_t floats_of(const amskv_rotary_spec* spec, int64_t rows)
+{
+    const int64_t d = spec->rotary_dim;
+    return rows < 1 || d < 1 ? 0 : rows > INT64_MAX / d ? INT64_MAX : rows * d;
+}
+
 /* rotary(spec, table, table_rows, first, index, index_row_stride, rows, T, head_dim, q_heads, Q, Q_out, k_heads, K, K_out, transposed, stream) */
 static PyObject* py_rotary(PyObject* self, PyObject* const* a, Py_ssize_t n)
 {
@@ -204,9 +263,9 @@ static PyObject* py_rotary(PyObject* self, PyObject* const* a, Py_ssize_t n)
     Py_buffer spec;
     if (count(n, 17)) return NULL;
     if (!PyObject_CheckBuffer(a[0]) || PyObject_GetBuffer(a[0], &spec, PyBUF_SIMPLE)) return left_to_ctypes();
-    if (spec.len != (Py_ssize_t)sizeof(amskv_rotary_spec) || tensor(a[1], &table, qs, &qv) || qv || as_int64(a[2], &table_rows) ||
-        as_int64(a[3], &first) || index_of(a[4], a[5], &index, &index_row) || as_int(a[6], &rows) || as_int(a[7], &T) || as_int(a[8], &d) ||
-        as_int(a[9], &qh) || tensor(a[10], &q, qs, &qv) || tensor(a[11], &qo, qos, &qov) || as_int(a[12], &kh) || tensor(a[13], &k, ks, &kv) ||
+    if (spec.len != (Py_ssize_t)sizeof(amskv_rotary_spec) || as_int64(a[2], &table_rows) ||
+        list_of(a[1], &torch_float32, "float32", floats_of(spec.buf, table_rows), &table) || as_int64(a[3], &first) || as_int(a[6], &rows) ||
+        as_int(a[7], &T) || index_of(a[4], a[5], rows, T, &index, &index_row) || as_int(a[8], &d) || as_int(a[9], &qh) || tensor(a[10], &q, qs, &qv) || tensor(a[11], &qo, qos, &qov) || as_int(a[12], &kh) || tensor(a[13], &k, ks, &kv) ||
         tensor(a[14], &ko, kos, &kov) || (a[15] != Py_True && a[15] != Py_False) || stream_of(a[16], &stream)) {
         PyBuffer_Release(&spec);
         return left_to_ctypes();
@@ -219,29 +278,26 @@ static PyObject* py_rotary(PyObject* self, PyObject* const* a, Py_ssize_t n)
     return PyLong_FromLong(rc);
 }
 
-/* address of a contiguous list of int32: None, an int or a tensor */
-static int list_of(PyObject* x, const int32_t** out)
-{
-    void* p;
-    int64_t s[3];
-    int strided;
-    if (tensor(x, &p, s, &strided) || strided) return -1;
-    *out = (const int32_t*)p;
-    return 0;
-}
-
 /* cross_attend(cache, scale, kv_heads, keys, K, V, Q, out, lengths, offsets, max_keys, stream) -> return code, or None */
 static PyObject* py_cross_attend(PyObject* self, PyObject* const* a, Py_ssize_t n)
 {
-    void *cache, *k, *v, *q, *o, *stream;
-    int64_t ks[3], qs[3], os[3];
+    void *cache, *k, *v, *q, *o, *stream, *lengths, *offsets;
+    int64_t ks[3], qs[3], os[3], shape[4], rows = 0;
     int scale, kv, qv, ov, rc, heads, keys, max_keys;
     amskv_encoder enc;
     if (count(n, 12)) return NULL;
     if (as_pointer(a[0], &cache) || as_int(a[1], &scale) || as_int(a[2], &heads) || as_int(a[3], &keys) || key_value(a[4], a[5], &k, &v, ks, &kv) ||
-        tensor(a[6], &q, qs, &qv) || tensor(a[7], &o, os, &ov) || list_of(a[8], &enc.lengths) || list_of(a[9], &enc.offsets) ||
-        as_int(a[10], &max_keys) || stream_of(a[11], &stream))
+        tensor(a[6], &q, qs, &qv) || tensor(a[7], &o, os, &ov) || as_int(a[10], &max_keys) || stream_of(a[11], &stream))
         return left_to_ctypes();
+    /* how many rows there are the queries tell, where they are a tensor */
+    if ((a[8] != Py_None || a[9] != Py_None) && a[6] != Py_None && !PyLong_CheckExact(a[6])) {
+        if (shape_of(a[6], shape, 4) != 4) return left_to_ctypes();
+        rows = shape[0];
+    }
+    if (list_of(a[8], &torch_int32, "int32", rows, &lengths) || list_of(a[9], &torch_int32, "int32", rows ? rows + 1 : 0, &offsets))
+        return left_to_ctypes();
+    enc.lengths = lengths;
+    enc.offsets = offsets;
     enc.kv_heads = heads;
     enc.keys = keys;
     enc.max_keys = max_keys;
@@ -289,6 +345,10 @@ PyMODINIT_FUNC PyInit__steps(void)
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_stride = PyUnicode_InternFromString("stride");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    if (!s_data_ptr || !s_is_contiguous || !s_stride || !s_cuda_stream) return NULL;
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_numel = PyUnicode_InternFromString("numel");
+    s_shape = PyUnicode_InternFromString("shape");
+    s_torch = PyUnicode_InternFromString("torch");
+    if (!s_data_ptr || !s_is_contiguous || !s_stride || !s_cuda_stream || !s_dtype || !s_numel || !s_shape || !s_torch) return NULL;
     return PyModule_Create(&module);
 }

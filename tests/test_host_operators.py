@@ -142,3 +142,24 @@ def test_promotion_of_a_layer_held_in_8_bits():
     assert B.amskv_resident_ranges(c, 0, 2) == [(0, 1), (16, 4), (32, 9)]
     assert np.isfinite(B.amskv_cache_bytes(c)).all()
     B.amskv_cache_destroy(c)
+
+
+@pytest.mark.parametrize("native", [True, False], ids=["native", "ctypes"])
+def test_lengths_and_offsets_that_the_kernels_would_misread(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(B, "_steps", None)
+    c = _plan()                                   # two rows
+    q = torch.zeros(2, 4, 4, 64, dtype=torch.bfloat16)
+    i32 = dict(dtype=torch.int32)
+    for kw in (dict(lengths=torch.zeros(2, **i32)), dict(lengths=torch.zeros(5, **i32)), dict(offsets=torch.zeros(3, **i32)), dict(lengths=A),
+               dict(offsets=torch.zeros(1, **i32), Q=3 * A), dict(lengths=None)):
+        assert _cross(c, **{**dict(Q=q), **kw}) == B.ERR_UNSUPPORTED, kw     # all is well, but there is no device memory
+    for kw in (dict(lengths=torch.zeros(2, dtype=torch.int64)), dict(lengths=torch.cumsum(torch.ones(2, **i32), 0)), dict(lengths=torch.zeros(2)),
+               dict(offsets=torch.zeros(3, dtype=torch.int64)), dict(lengths=torch.zeros(1, **i32)), dict(lengths=torch.zeros(0, **i32)),
+               dict(offsets=torch.zeros(2, **i32)), dict(lengths=torch.zeros(2, dtype=torch.int16))):
+        for queries in (q, q.transpose(1, 2).contiguous().transpose(1, 2)):
+            with pytest.raises(ValueError):
+                B.amskv_cross_attend(c, 1, 2, 7, A, 2 * A, queries, 4 * A, **kw)
+    with pytest.raises(ValueError):
+        B.amskv_cross_attend(c, 1, 2, 7, A, 2 * A, 3 * A, 4 * A, lengths=torch.zeros(2, dtype=torch.int64))
+    B.amskv_cache_destroy(c)

@@ -108,3 +108,47 @@ def test_what_the_native_module_serves_and_what_it_leaves_to_ctypes():
         assert B._steps.cross_attend(*cross[:at], value, *cross[at + 1:]) is None, at
     with pytest.raises(TypeError):
         B._steps.rotary(spec)
+
+
+@pytest.mark.parametrize("native", [True, False], ids=["native", "ctypes"])
+def test_lists_and_tables_that_the_kernels_would_misread(native, monkeypatch):
+    """Of another type, with gaps, or too short: refused before the library is called.  What is right gets as far as the library, which
+    here refuses something else (no launch can follow either way)."""
+    if not native:
+        monkeypatch.setattr(B, "_steps", None)
+    spec, x = B.make_rotary(64, axes=2), torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16)
+
+    def rotary(table=A, index=None, rows=2, T=4, **kw):
+        B.amskv_rotary(spec, table, 16, 0, index, rows, T, 60, 3, x, x, **kw)      # head_dim 60: below rotary_dim
+
+    i32 = dict(dtype=torch.int32)
+    for kw in (dict(table=torch.zeros(16, 32, 2)), dict(table=torch.zeros(20, 64)), dict(index=torch.zeros(4, **i32)), dict(index=torch.zeros(9, **i32)),
+               dict(index=torch.zeros(2, 4, **i32)), dict(index=torch.zeros(3, 9, **i32)[:, 2:7]), dict(index=torch.zeros(1, 4, **i32), rows=1),
+               dict(index=torch.zeros(1, 4, **i32).expand(2, 4)), dict(index=torch.zeros(8, **i32), index_row_stride=4),
+               dict(index=torch.zeros(1, 4, **i32), index_row_stride=0), dict(index=torch.zeros(2, 5, **i32)[:, :4], index_row_stride=5),
+               dict(index=torch.zeros(2, 4, 1, **i32)[:, :, 0].t()[:1].t(), T=1)):
+        with pytest.raises(B.AmskvError) as e:
+            rotary(**kw)
+        assert e.value.code == B.ERR_INVALID, kw
+    for kw in (dict(table=torch.zeros(16, 32, 2).double()), dict(table=torch.zeros(16, 64, 2)[:, ::2]), dict(table=torch.zeros(15, 32, 2)),
+               dict(table=x), dict(index=torch.zeros(4, dtype=torch.int64)), dict(index=torch.zeros(4)), dict(index=torch.zeros(3, **i32)),
+               dict(index=torch.zeros(0, **i32)), dict(index=torch.zeros(1, 4, **i32)), dict(index=torch.zeros(2, 3, **i32)),
+               dict(index=torch.zeros(2, 4, dtype=torch.int16)), dict(index=torch.zeros(8, **i32), index_row_stride=5),
+               dict(index=torch.zeros(2, 4, **i32), index_row_stride=8)):
+        with pytest.raises(ValueError):
+            rotary(**kw)
+    for bad in (dict(first=1 << 63), dict(table_rows=1 << 63), dict(index=A, index_row_stride=1 << 63)):
+        with pytest.raises(OverflowError):
+            B.amskv_rotary(**{**dict(spec=spec, table=A, table_rows=16, first=0, index=None, rows=2, T=4, head_dim=60, q_heads=3, Q=A, Q_out=A), **bad})
+
+    positions, table = torch.zeros(16, 2), torch.zeros(16, 32, 2)
+    with pytest.raises(B.AmskvError) as e:
+        B.amskv_rotary_table(B.make_rotary(64, axes=2, base=0.5), positions, 16, table)     # refused for its base
+    assert e.value.code == B.ERR_INVALID
+    for p, t in ((positions.double(), table), (positions.int(), table), (torch.zeros(2, 16).t(), table), (torch.zeros(16, 1).expand(16, 2), table),
+                 (positions[:15], table), (torch.zeros(16, 3)[:, :2], table), (positions, table.double()), (positions, table[:15]),
+                 (positions, torch.zeros(16, 64, 2)[:, ::2])):
+        with pytest.raises(ValueError):
+            B.amskv_rotary_table(spec, p, 16, t)
+    with pytest.raises(OverflowError):
+        B.amskv_rotary_table(spec, A, 1 << 64, A)
