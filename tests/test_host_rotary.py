@@ -152,3 +152,16 @@ def test_lists_and_tables_that_the_kernels_would_misread(native, monkeypatch):
             B.amskv_rotary_table(spec, p, 16, t)
     with pytest.raises(OverflowError):
         B.amskv_rotary_table(spec, A, 1 << 64, A)
+
+
+@pytest.mark.skipif(B._steps is None, reason="the native module is not built")
+def test_keys_as_an_address_and_values_as_a_tensor():
+    """Served where the tensor is contiguous, as an address is taken to be; refused where it is a view."""
+    x = torch.zeros(2, 2, 4, 64, dtype=torch.bfloat16)
+    for k, v in ((A, x), (x, A), (A, A)):
+        assert B._steps.cross_attend(None, 0, 1, 7, k, v, x, x, None, None, 0, None) == B.ERR_INVALID      # no cache
+    view = x.transpose(0, 1)
+    for k, v in ((view, A), (A, view), (view, x)):
+        assert B._steps.cross_attend(None, 0, 1, 7, k, v, x, x, None, None, 0, None) is None
+        with pytest.raises(ValueError):
+            B.amskv_cross_attend(None, 0, 1, 7, k, v, x, x)
