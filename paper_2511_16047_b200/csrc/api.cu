@@ -277,11 +277,19 @@ void note_appended(amskv_cache* cache, int layer, int scale)
 //   128 channels, an encoder:  T = 16  512 12.2 / 16.5, 8 192 184 / 205 (77 keys 127 / 111);  T = 64  128 9.3 / 9.6 (512 keys 15.0 / 13.5, 1 024 21.5 / 23.5),
 //     512 26.2 / 17.5;  T = 100  32 6.7 / 9.3, 64 8.5 / 9.3;  T = 144  16 5.1 / 8.2, 32 6.7 / 8.2, 64 11.5 / 8.5;  T = 256  16 6.7 / 8.9, 32 8.5 / 9.0
 //   128 channels, 8 bits:      T = 36  128 11.3 / 13.1, 512 30.4 / 23.8;  T = 100  32 11.6 / 15.4, 64 13.6 / 15.4, 128 21.1 / 15.7;  T = 144  16 12.6 / 12.3, 32 14.8 / 12.5
+// Grouped heads: the warp-matrix kernel's blocks hold the rows of a whole group, a tile of the other those of one head, so that few queries
+// a head leave it empty however many heads share a key.  us per call, an encoder, 256 keys, groups of 2, 4, 8:
+//   64 channels:   T = 4  640 items 8.7 / 20.7, 8.7 / 32.3, 11.0 / 55.3;  T = 16  160 5.7 / 9.3, 8.1 / 14.5, 12.7 / 20.9,
+//     1 600 25.4 / 39.5, 39.8 / 68.0, 66.5 / 131;  T = 25  640 16.8 / 21.2, 27.2 / 33.0, 48.3 / 57.0, 1 600 38.9 / 40.3, 62.7 / 69.5, 113 / 133;
+//     T = 36  1 600 55.6 / 41.2, 84.8 / 71.7, 145 / 137
+//   128 channels:  T = 16  640 22.5 / 26.7, 34.0 / 45.0, 56.9 / 82.3, 1 600 50.1 / 56.2, 70.0 / 102, 124 / 193;
+//     T = 25  640 33.1 / 28.1, 54.1 / 45.5, 93.4 / 82.8
 bool takes_tiles(const amskv_cache* cache, int32_t T, int32_t group, int64_t items, int64_t keys)
 {
     if (!cache->tc_ready || cache->path == AMSKV_PATH_SMALL || cache->path == AMSKV_PATH_SIMT) return false;
     if (cache->path != AMSKV_PATH_AUTO) return true;
     const int64_t M = (int64_t)T * group, sms = cache->sm_count, ctas = items * ((M + 63) / 64);
+    if (group > 1 && T <= (cache->head_dim == 64 ? 25 : 16)) return false;
     if (M <= 16) return items > 16 * sms && keys <= 256;
     if (M <= 32 && items <= 4 * sms) return false;
     if (cache->head_dim == 64) return ctas > 2 * sms && !(cache->held() && M <= 64 && items <= 16 * sms);

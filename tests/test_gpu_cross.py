@@ -319,3 +319,25 @@ def test_a_path_of_ones_own_choice_depends_on_the_shapes_alone(D, kv, side, keys
 def test_clusters_that_share_long_keys(shape):
     """Two, four and eight CTAs to a row's keys, which only calls of few items under AUTO have."""
     test_rows_of_different_lengths(shape, "auto")
+
+
+@pytest.mark.parametrize("D,group,side,rows,tiles", [
+    (64, 8, 2, 80, False), (64, 2, 4, 200, False), (64, 4, 3, 40, False), (64, 8, 5, 80, False), (64, 4, 6, 200, True), (64, 1, 6, 200, True),
+    (128, 8, 2, 80, False), (128, 2, 4, 80, False), (128, 8, 4, 200, False), (128, 4, 5, 80, True), (128, 4, 10, 80, True)])
+def test_few_queries_of_grouped_heads_share_a_block(D, group, side, rows, tiles):
+    """Which kernel AUTO takes, told by the bits of its outputs: a tile of 128 rows holds one head's queries, a block of the
+    warp-matrix kernel those of all heads that share a key."""
+    kv, keys = 8, 200
+    g = torch.Generator(device="cuda").manual_seed(group)
+    q = torch.randn(rows, kv * group, side * side, D, generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn(rows, kv, keys, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    outs = []
+    with Cache(1, kv * group, D, rows, (side,), [(0, 1, False)]) as c:
+        for path in (B.PATH_AUTO, B.PATH_TENSOR_PAIR):
+            B.amskv_set_attend_path(c.h, path)
+            outs.append(torch.zeros_like(q))
+            B.amskv_cross_attend(c.h, 0, kv, keys, k, v, q, outs[-1])
+        assert B.amskv_status(c.h) == 0
+    assert torch.equal(*outs) == tiles
+    at = [0, rows - 1]
+    _check(outs[0][at], q[at], [(_np(k[r]), _np(v[r])) for r in at], group, 1.0 / math.sqrt(D), "grouped")
