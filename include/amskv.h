@@ -504,8 +504,9 @@ AMSKV_API int amskv_rotary_table_bytes(const amskv_rotary_spec* spec, int64_t co
 
 /*
  * Fills a table: row n holds amplitude * (cos, sin) of the angles of position n, columns in axis-major order.  Made once for
- * a schedule (its scales one behind the other, say); angles are formed to 2^-32 of a turn, however far the position, and a position that
- * is not a finite number gives entries that are not numbers.
+ * a schedule (its scales one behind the other, say); angles are formed to 2^-31 of a turn and, frequencies being
+ * doubles, 2^-50 of the angle and 2^-64 of a turn per unit of position on top (1e-9 of a turn at position 10^6, 10^-5 at 10^11; from 10^15 on
+ * nothing is left).  A position that is not a finite number gives entries that are not numbers.
  *   positions   device pointer to count * axes floats, 4-byte aligned
  *   table       device pointer, amskv_rotary_table_bytes() bytes, 16-byte aligned
  * Enqueued on `stream`.  Errors: INVALID, CUDA.

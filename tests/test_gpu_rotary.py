@@ -3,6 +3,9 @@
 Tolerances.  A table entry: the angle, rounded twice, is right to 2^-23 of at most pi / 4, the sums to two units of 2^-24, the
 amplitude's product to one more: under 2^-21.  An output: three fp32 roundings of |u| + |w| times the amplitude
 and the table's error times the same, under 2^-20 of it together, then half a step of bf16, 2^-8 of the value."""
+import decimal
+from decimal import Decimal
+
 import numpy as np
 import pytest
 import torch
@@ -212,3 +215,31 @@ def test_a_token_without_a_position_is_passed_on_bit_for_bit(rows, heads, T, D, 
         out = x if in_place else torch.zeros_like(x)
         B.amskv_rotary(spec, table, 4, 0, index, rows, T, D, heads, x, out, transposed=transposed)
         assert torch.equal(out.view(torch.int16), bits)
+
+
+def _exact_entries(positions, dim, base):
+    """Cosines and sines by decimal arithmetic of 90 digits, and the angles."""
+    with decimal.localcontext() as ctx:
+        ctx.prec = 90
+        pi = sum((Decimal(4) / (8 * n + 1) - Decimal(2) / (8 * n + 4) - Decimal(1) / (8 * n + 5) - Decimal(1) / (8 * n + 6)) / 16 ** n for n in range(75))
+        out, angles = np.empty((len(positions), dim // 2, 2)), np.empty((len(positions), dim // 2))
+        for i in range(dim // 2):
+            w = (Decimal(-2 * i) / dim * Decimal(base).ln()).exp()
+            for n, p in enumerate(positions):
+                angle = Decimal(p) * w
+                rest = float(angle - 2 * pi * (angle / (2 * pi)).to_integral_value())
+                out[n, i], angles[n, i] = (np.cos(rest), np.sin(rest)), float(angle)
+        return out, angles
+
+
+@pytest.mark.parametrize("dim,base", [(64, 10000.0), (128, 500000.0), (12, 3.0)])
+def test_far_positions_against_many_digits(dim, base):
+    """To what the header promises: 2^-31 of a turn, 2^-50 of the angle and 2^-64 of a turn per unit of position, and an entry's own
+    2^-21."""
+    pos = torch.tensor([[1.0], [0.3], [8191.25], [1e6], [2.0 ** 23 - 0.5], [2.0 ** 24 + 2], [-2.0 ** 28 - 32], [2.0 ** 31], [1e11], [-7e12], [1e15]])
+    got = _table(B.make_rotary(dim, base=base), dim, pos.cuda())[:len(pos)].cpu().double().numpy()
+    want, angles = _exact_entries([float(p) for p in pos[:, 0]], dim, base)
+    at = pos[:, :1].abs().double().numpy()
+    tol = 2.0 ** -21 + 2 * np.pi * (2.0 ** -31 + at * 2.0 ** -64) + np.abs(angles) * 2.0 ** -50
+    assert (np.abs(got - want) <= tol[..., None]).all()
+    assert (tol[:9] < 2e-4).all()
