@@ -638,7 +638,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
         };
         if (q_loader) {
             prefetch_tensormap(&q_map);
-            prefetch_tensormap(&o_map);
+            if (C::kBulkOut) prefetch_tensormap(&o_map);
             if (!C::kLoaderQ) load_next_q(bounds_at(0));
         }
         __syncwarp();
@@ -900,8 +900,9 @@ cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, c
     int pos[3];
     if (!tc_encode_q_map(Q, T, rows, plan.heads, D, kQRows, &qm, pos)) return cudaErrorNotSupported;
     CUtensorMap om, km, vm, vm16;
-    int opos[3], kpos[3] = {1, 2, 3}, vpos[3] = {1, 2, 3};
-    if (!tc_encode_q_map(O, T, rows, plan.heads, D, kOutRows, &om, opos)) return cudaErrorNotSupported;
+    int opos[3] = {1, 2, 3}, kpos[3] = {1, 2, 3}, vpos[3] = {1, 2, 3};
+    memset(&om, 0, sizeof(om));
+    if (C::kBulkOut && !tc_encode_q_map(O, T, rows, plan.heads, D, kOutRows, &om, opos)) return cudaErrorNotSupported;
     memset(&km, 0, sizeof(km));
     memset(&vm, 0, sizeof(vm));
     memset(&vm16, 0, sizeof(vm16));
