@@ -407,10 +407,10 @@ cudaError_t launch(const Strided& Q, const Strided& O, const EncoderKeys& enc, c
     const cudaError_t oe = opt_in.ensure(attend_rows_kernel<D, kQB, kHeld, kWarps>, C::kSmemBytes);
     if (oe != cudaSuccess) return oe;
     const int64_t blocks = ((int64_t)T * group + 15) / 16, parts = (blocks + kQB - 1) / kQB, ctas = parts * rows * kv_heads;
-    // Few CTAs and several chunks of keys: clusters share them.  What a merge costs is about four chunks of an encoder's keys (in CTAs of
-    // 64 rows more) or two of codes (256 keys in four chunks, shared by two CTAs / not: 64 channels 5.4 / 4.6, 128 channels 7.5 / 6.7 us;
+    // Few CTAs and several chunks of keys: clusters share them.  What a merge costs is about four chunks of an encoder's keys or
+    // two of codes (256 keys in four chunks, shared by two CTAs / not: 64 channels 5.4 / 4.6, 128 channels 7.5 / 6.7 us;
     // 484 keys 6.2 / 6.7 and 9.0 / 9.8; 8 bits, 64 channels, 256 keys 6.2 / 7.6).
-    constexpr int kFirst = kHeld ? 4 : 8, kMore = kQB == 4 && !kHeld ? 8 : 4;
+    constexpr int kFirst = kHeld ? 4 : 8, kMore = 4;
     const int64_t chunks = (max_keys + kChunk - 1) / kChunk;
     int32_t splits = 1;
     const int64_t slots = kWarps == 8 && D == 128 ? sm_count : 2ll * sm_count;   // (a CTA of eight warps of 128 channels has an SM's registers)
