@@ -269,7 +269,8 @@ void note_appended(amskv_cache* cache, int layer, int scale)
 
 // Whether the tensor-memory kernel (attend_tiles.cu) serves a call over an encoder's states or a cache held in 8 bits, else the
 // warp-matrix kernel (attend_rows.cu), which wins where its CTAs of up to 64 query rows all run at once, sharing long keys
-// between them, and where 16 rows or fewer leave the other's tiles of 128 empty.  `items`: rows x key/value heads; `group` query heads share one.
+// between them, and where 16 rows or fewer leave the other's tiles of 128 empty.  `codes`: the keys are a cache's held in 8 bits (which an
+// encoder's are not, whatever the cache of the call holds); `items`: rows x key/value heads; `group` query heads share one.
 // us per call, warp-matrix / tensor-memory, in a graph, 256 keys where nothing else is said:
 //   64 channels, an encoder:   T = 16  512 items 6.6 / 10.2, 8 192 88 / 99 (77 keys 67 / 60);  T = 36  128 6.3 / 8.9, 512 11.8 / 10.6;
 //     T = 100  128 8.2 / 9.0, 512 24.5 / 12.4;  T = 144  32 4.6 / 8.5, 128 11.1 / 8.7;  T = 256  32 5.7 / 9.0, 64 8.2 / 9.0
@@ -284,7 +285,7 @@ void note_appended(amskv_cache* cache, int layer, int scale)
 //     T = 36  1 600 55.6 / 41.2, 84.8 / 71.7, 145 / 137
 //   128 channels:  T = 16  640 22.5 / 26.7, 34.0 / 45.0, 56.9 / 82.3, 1 600 50.1 / 56.2, 70.0 / 102, 124 / 193;
 //     T = 25  640 33.1 / 28.1, 54.1 / 45.5, 93.4 / 82.8
-bool takes_tiles(const amskv_cache* cache, int32_t T, int32_t group, int64_t items, int64_t keys)
+bool takes_tiles(const amskv_cache* cache, bool codes, int32_t T, int32_t group, int64_t items, int64_t keys)
 {
     if (!cache->tc_ready || cache->path == AMSKV_PATH_SMALL || cache->path == AMSKV_PATH_SIMT) return false;
     if (cache->path != AMSKV_PATH_AUTO) return true;
@@ -292,8 +293,8 @@ bool takes_tiles(const amskv_cache* cache, int32_t T, int32_t group, int64_t ite
     if (group > 1 && T <= (cache->head_dim == 64 ? 25 : 16)) return false;
     if (M <= 16) return items > 16 * sms && keys <= 256;
     if (M <= 32 && items <= 4 * sms) return false;
-    if (cache->head_dim == 64) return ctas > 2 * sms && !(cache->held() && M <= 64 && items <= 16 * sms);
-    return ctas > sms || (M > 128 && (cache->held() || items * ((M + 15) / 16) > 2 * sms));
+    if (cache->head_dim == 64) return ctas > 2 * sms && !(codes && M <= 64 && items <= 16 * sms);
+    return ctas > sms || (M > 128 && (codes || items * ((M + 15) / 16) > 2 * sms));
 }
 
 // which kernel amskv_attend uses for T query tokens over `total` keys
@@ -510,7 +511,7 @@ int amskv_attend(amskv_cache* cache, int layer, int scale, const void* Q, void* 
         HeldKeys keys{region.codes, region.scales, region.capacity, 0, ranges};
         for (int i = 0; i < ranges.n; ++i) keys.blocks += (ranges.r[i].len + kBlock - 1) / kBlock;
         e = cudaErrorNotSupported;
-        if (takes_tiles(cache, T, 1, cache->items(), (int64_t)keys.blocks * kBlock))
+        if (takes_tiles(cache, true, T, 1, cache->items(), (int64_t)keys.blocks * kBlock))
             e = launch_attend_tiles(q, o, keys, T, cache->rows, cache->heads, cache->head_dim, cache->softmax_scale, cache->status_word(),
                                     cache->sm_count, static_cast<cudaStream_t>(stream));
         if (e == cudaErrorNotSupported)   // (strides that no tensor map holds, too)
@@ -846,7 +847,7 @@ int amskv_cross_attend(amskv_cache* cache, int scale, const amskv_encoder* enc, 
                            kv_rows == cache->rows && k.row != 0 && !enc->offsets};
     const int32_t group = cache->heads / enc->kv_heads;
     cudaError_t e = cudaErrorNotSupported;
-    if (takes_tiles(cache, T, group, (int64_t)cache->rows * enc->kv_heads, keys.max_keys))
+    if (takes_tiles(cache, false, T, group, (int64_t)cache->rows * enc->kv_heads, keys.max_keys))
         e = launch_attend_tiles(q, o, keys, T, cache->rows, enc->kv_heads, group, cache->head_dim, cache->softmax_scale, cache->status_word(),
                                 cache->sm_count, static_cast<cudaStream_t>(stream));
     if (e == cudaErrorNotSupported)   // (strides that no tensor map holds, too)

@@ -341,3 +341,19 @@ def test_few_queries_of_grouped_heads_share_a_block(D, group, side, rows, tiles)
     assert torch.equal(*outs) == tiles
     at = [0, rows - 1]
     _check(outs[0][at], q[at], [(_np(k[r]), _np(v[r])) for r in at], group, 1.0 / math.sqrt(D), "grouped")
+
+
+@pytest.mark.parametrize("D,heads,side,rows", [(64, 8, 8, 100), (64, 8, 6, 100), (128, 4, 13, 3), (128, 4, 16, 2), (64, 4, 1, 2)])
+def test_what_the_cache_holds_makes_no_difference(D, heads, side, rows):
+    """Cross attention takes the kernel that an encoder's keys are best served by, beside a cache of 8 bits as beside any other."""
+    keys = 200
+    g = torch.Generator(device="cuda").manual_seed(side)
+    q = torch.randn(rows, heads, side * side, D, generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn(rows, heads, keys, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    outs = []
+    for flags in (0, B.FLAG_KV_E4M3):
+        with Cache(1, heads, D, rows, (side,), [(0, 1, False)], flags=flags) as c:
+            outs.append(torch.zeros_like(q))
+            B.amskv_cross_attend(c.h, 0, heads, keys, k, v, q, outs[-1])
+            assert B.amskv_status(c.h) == 0
+    assert torch.equal(*outs)
