@@ -836,6 +836,8 @@ int amskv_cross_attend(amskv_cache* cache, int scale, const amskv_encoder* enc, 
     Strided k, v, q, o;
     // (packed keys have no row dimension; the same keys for all rows, a row stride of 0, are read as they are)
     const int32_t kv_rows = enc->offsets || (kv_strides && kv_strides[0] == 0) ? 1 : cache->rows;
+    const int64_t packed_strides[3] = {0, kv_strides ? kv_strides[1] : 0, kv_strides ? kv_strides[2] : 0};   // (whatever their row stride is)
+    if (enc->offsets && kv_strides) kv_strides = packed_strides;
     int rc = make_strided(K, kv_strides, kv_rows, enc->kv_heads, enc->keys, cache->head_dim, &k);
     if (rc == AMSKV_OK) rc = make_strided(V, kv_strides, kv_rows, enc->kv_heads, enc->keys, cache->head_dim, &v);
     if (rc == AMSKV_OK) rc = make_strided(Q, q_strides, cache->rows, cache->heads, T, cache->head_dim, &q);

@@ -163,3 +163,19 @@ def test_lengths_and_offsets_that_the_kernels_would_misread(native, monkeypatch)
     with pytest.raises(ValueError):
         B.amskv_cross_attend(c, 1, 2, 7, A, 2 * A, 3 * A, 4 * A, lengths=torch.zeros(2, dtype=torch.int64))
     B.amskv_cache_destroy(c)
+
+
+def test_the_row_stride_of_packed_keys_is_not_looked_at():
+    c = _plan()
+    kv = torch.zeros(4096, dtype=torch.bfloat16)
+    for row in (3, 0, 1 << 20):
+        x = torch.as_strided(kv, (1, 2, 7, 64), (row, 64, 128, 1))
+        assert _cross(c, K=x, V=x, offsets=A) == B.ERR_UNSUPPORTED       # all is well, but there is no device memory
+    strides = (B.ctypes.c_int64 * 3)(-8, 64, 128)
+    enc = B.Encoder(2, 7, 0, None, A)
+    assert B.lib.amskv_cross_attend(c, 1, B.ctypes.byref(enc), A, A, strides, A, 2 * A, None, None, None) == B.ERR_UNSUPPORTED
+    x = torch.as_strided(kv, (1, 2, 7, 64), (3, 64, 128, 1))
+    assert _cross(c, K=x, V=x) == B.ERR_INVALID                          # padded keys: it is
+    x = torch.as_strided(kv, (1, 2, 7, 64), (0, 0, 128, 1))
+    assert _cross(c, K=x, V=x, offsets=A) == B.ERR_INVALID               # a head repeated
+    B.amskv_cache_destroy(c)
