@@ -310,7 +310,8 @@ AMSKV_API int amskv_read_segment(amskv_cache* cache, int layer, int segment, voi
  *   max_keys  the most keys that a row has (0: `keys`); rows with more are cut to it.  It decides launch shapes: give the batch's
  *             longest length where offsets are used.
  *   kv_heads  divides heads: query head h reads key/value head h / (heads / kv_heads).
- *   Q, out    as for amskv_attend.  out must not overlap any input.  A row without keys gets zeros.
+ *   Q, out    as for amskv_attend.  out must not overlap any input.  A row without keys gets zeros, and so
+ *             does a query all of whose scores are minus infinity.
  * Path: AMSKV_PATH_SMALL and AMSKV_PATH_SIMT are the warp-matrix kernel, AMSKV_PATH_TENSOR and AMSKV_PATH_TENSOR_PAIR the tensor-memory
  * kernel.  Arithmetic as for amskv_attend; the sums of probabilities times values are formed in fp32 up to 2^24 times, or down to 2^-40 times,
  * what they are in the end, so that |V| times the number of keys has to stay below 2^104, and outputs below 2^-60 lose digits.  A NaN goes where the

@@ -739,29 +739,29 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                         return sum0 + sum1;
                     };
                     float tile_sum = exp_tile();
-                    if (j > 0) {
-                        // (the polynomial ends at 2^126, so that it cannot hide a row that has outgrown its reference)
-                        const bool over = !(tile_sum <= kSumLimit);
-                        if (__any_sync(0xffffffffu, over)) {
-                            // Rare.  The P V before must be done: with one S buffer it was issued before this S, whose arrival covers it; with two it
-                            // has an arrival of its own (the next one needs the P that this tile has not announced yet).
-                            if (C::kSBufs == 2) {
-                                if (!__all_sync(0xffffffffu, mbar_wait(pv_done0 + 8 * g, (t - 1u) & 1u, abort_flag))) {
-                                    report(status, kStatusSyncTimeout, abort_flag);
-                                    ok = false;
-                                    break;
-                                }
-                                tc_fence_after();
+                    // (the polynomial ends at 2^126, so that it cannot hide a row that has outgrown its reference)
+                    const bool over = !(tile_sum <= kSumLimit);
+                    if (__any_sync(0xffffffffu, over)) {
+                        // Rare.  The P V before must be done: with one S buffer it was issued before this S, whose arrival covers it; with two it
+                        // has an arrival of its own (the next one needs the P that this tile has not announced yet).
+                        if (C::kSBufs == 2 && j > 0) {
+                            if (!__all_sync(0xffffffffu, mbar_wait(pv_done0 + 8 * g, (t - 1u) & 1u, abort_flag))) {
+                                report(status, kStatusSyncTimeout, abort_flag);
+                                ok = false;
+                                break;
                             }
-                            tmem_wait_st();
-                            const float mt = tile_max();
-                            float alpha = 1.f;
-                            if (over || fmaf(mt, scale_log2, nb) > kRescaleLog2 - kLowered) {
-                                alpha = fast_exp2((m_ref - mt) * scale_log2);
-                                m_ref = mt;
-                                nb = fmaf(-mt, scale_log2, -kLowered);
-                                l *= alpha;
-                            }
+                            tc_fence_after();
+                        }
+                        tmem_wait_st();
+                        const float mt = tile_max();
+                        float alpha = 1.f;
+                        if (over || fmaf(mt, scale_log2, nb) > kRescaleLog2 - kLowered) {
+                            if (m_ref != mt) alpha = fast_exp2((m_ref - mt) * scale_log2);
+                            m_ref = mt;
+                            nb = mt == -INFINITY ? -kLowered : fmaf(-mt, scale_log2, -kLowered);
+                            l *= alpha;
+                        }
+                        if (j > 0) {
 #pragma unroll 1
                             for (int cb = 0; cb < D / 8; ++cb) {
                                 uint32_t o[8];
@@ -770,8 +770,11 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                                 for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
                                 tmem_st8(o_tmem + cb * 8, o);
                             }
-                            tile_sum = exp_tile();
                         }
+                        tile_sum = exp_tile();
+                        // Scores of minus infinity alone so far: probabilities and a sum of 0.  An infinite term makes the next tile's sum infinite or no
+                        // number, whatever its scores are, and brings the row here again.
+                        if (m_ref == -INFINITY) nb = INFINITY;
                     }
                     l += tile_sum;
                     tmem_wait_st();
@@ -792,7 +795,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
                 tc_fence_after();
             }
             if (!C::kBulkOut && warp_live && n_tiles > 0) {
-                const float inv = 1.f / l;
+                const float inv = l > 0.f ? 1.f / l : 0.f;   // (no key but those of minus infinity: zeros)
                 __nv_bfloat16* dst = O + u.row * o_row + u.head(g) * o_head + (int64_t)(u.qt(g) * kQRows + r) * o_tok;
 #pragma unroll
                 for (int cb = 0; cb < D / 32; ++cb) {
@@ -818,7 +821,7 @@ attend_tiles_kernel(const __grid_constant__ CUtensorMap q_map, int3 qpos, const 
             } else if (warp_live && n_tiles > 0) {
                 // Through the place of the unit's queries, which nobody reads any more, and out as one bulk copy per 64 channels: stores straight
                 // from the registers, a row per thread, take a memory transaction for every 32 bytes.  Rows past T are outside the tensor.
-                const float inv = 1.f / l;
+                const float inv = l > 0.f ? 1.f / l : 0.f;   // (no key but those of minus infinity: zeros)
                 const uint32_t place = q_smem + (g * C::kQBufs + qbuf_of(un - 1u)) * C::kQBytes + wq * 32 * 128;
                 uint8_t* mine = smem_raw + (place - raw) + lane * 128;
                 constexpr int kCols = kHeld ? 32 : 64;   // (as many at a time as there are registers for)

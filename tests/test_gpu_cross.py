@@ -357,3 +357,29 @@ def test_what_the_cache_holds_makes_no_difference(D, heads, side, rows):
             B.amskv_cross_attend(c.h, 0, heads, keys, k, v, q, outs[-1])
             assert B.amskv_status(c.h) == 0
     assert torch.equal(*outs)
+
+
+@pytest.mark.parametrize("path", sorted(PATHS))
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("after", [0.0, -500.0, 30.0])
+@pytest.mark.parametrize("masked", [1, 63, 64, 130])
+def test_scores_of_minus_infinity(masked, after, path, D):
+    """Keys masked by an infinity in one channel: tiles of nothing else first, logits of any size behind them, and masked keys among those."""
+    rows, heads, side, keys = 2, 2, 12, 200
+    g = torch.Generator(device="cuda").manual_seed(masked)
+    q = torch.randn(rows, heads, side * side, D, generator=g, device="cuda")
+    k, v = (torch.randn(rows, heads, keys, D, generator=g, device="cuda") for _ in range(2))
+    q[..., 0], q[..., 1], k[..., 0], k[..., 1] = 1.0, 1.0, 0.0, after * math.sqrt(D)
+    real = torch.ones(keys, dtype=torch.bool)
+    real[:masked] = real[150:160] = False
+    k[:, :, ~real, 0] = -float("inf")
+    q, k, v = (x.bfloat16() for x in (q, k, v))
+    with Cache(1, heads, D, rows, (side,), [(0, 1, False)]) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+        out = torch.full_like(q, float("nan"))
+        B.amskv_cross_attend(c.h, 0, heads, keys, k, v, q, out)
+        assert B.amskv_status(c.h) == 0
+        _check(out, q, [(_np(k[r][:, real]), _np(v[r][:, real])) for r in range(rows)], 1, 1.0 / math.sqrt(D), "masked")
+        k[..., 0] = -float("inf")                            # of all keys: none is left, and the row gets zeros
+        B.amskv_cross_attend(c.h, 0, heads, keys, k, v, q, out)
+        assert B.amskv_status(c.h) == 0 and (out == 0).all()
