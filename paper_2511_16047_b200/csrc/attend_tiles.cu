@@ -20,7 +20,8 @@
 // come in bulk copies into a ring of tiles, from which warps widen them to bf16; where a tile's codes lie, and which of its slots
 // hold a key, is tabulated once per launch.
 // What bounds it: the exponentials, 64 channels (a tile's 8 192 take 512 cycles of an SM's special-function unit, the products 256), and
-// the products, 128 channels; with codes of 64 channels the issue slots that softmax and widening share.  4 096 queries x 10 521 keys x 64
+// the products, 128 channels; with codes no unit by itself (64 channels: special-function unit 46 %, issue slots 44 % busy at 425 keys), but the
+// chain of widening, S, softmax and P V, whose waits for tensor memory lead.  4 096 queries x 10 521 keys x 64
 // heads: 64 channels 910 us (0.73 PFLOP/s of products), 128 channels 1 050 (1.26); from codes 1 040 to 1 270 and 1 250 (0.9 and 1.06).
 // 256 queries x 430 keys: 64 channels, 3 840 heads 179, codes 225; 128 channels, 2 048 heads 143, codes 175.
 // Every wait is bounded: one that gives up records a status code and sets a flag, its role stops, and so do the others at their

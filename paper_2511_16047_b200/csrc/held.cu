@@ -32,7 +32,7 @@ __device__ __forceinline__ uint2 codes_of(const uint4& x, __nv_bfloat162 inv)
 }
 
 // A warp per block of K or of V, which needs half the registers of one for both and leaves twice the warps to wait for memory (256 items,
-// 1 024 tokens, 128 channels: 37.7 us, 29.0; 30.8 at the rate of a copy).  Divisions by launch constants are multiplications.
+// 1 024 tokens, 128 channels: 37.7 us, 29.1; 30.8 at the rate of a copy).  Divisions by launch constants are multiplications.
 template <int D>
 __global__ void __launch_bounds__(kThreads)
 append_held_kernel(const __nv_bfloat16* K, const __nv_bfloat16* V, int64_t k_row, int64_t k_head, int64_t k_tok, int64_t v_row,

@@ -200,7 +200,9 @@ rotary_kernel(const __grid_constant__ RotaryArgs a, int32_t units)
 }
 
 // Any shape: tokens go through shared memory, so that a thread, which writes eight channels, finds their partners wherever they are.
-// Everything a block writes it has read before, so that the output may be the input.
+// Everything a block writes it has read before, so that the output may be the input.  What bounds it: an 8-byte load of the table per channel,
+// which heads do not share, and two barriers per 4 KB.  16 rows x 32 heads x 4 096 x 128: 616 us with 120 channels turned by halves or
+// 124 interleaved, where the kernel above takes 158 with 112, 120 (interleaved) or 128.
 __global__ void __launch_bounds__(kThreads)
 rotary_any_kernel(const __grid_constant__ RotaryArgs a)
 {
