@@ -383,3 +383,25 @@ def test_scores_of_minus_infinity(masked, after, path, D):
         k[..., 0] = -float("inf")                            # of all keys: none is left, and the row gets zeros
         B.amskv_cross_attend(c.h, 0, heads, keys, k, v, q, out)
         assert B.amskv_status(c.h) == 0 and (out == 0).all()
+
+
+@pytest.mark.parametrize("path", ["rows", "tiles"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("spread", [0.3, 1.0, 4.0])
+def test_errors_in_the_mean_are_those_of_two_roundings(spread, D, path):
+    """Root mean square over all outputs.  A bf16 rounding is off by up to 2^-8 / m of a number m 2^e, evenly: in the mean over mantissas
+    spread as those of products are, 2^-8 * 0.735 / sqrt(3) = 0.85 * 2^-9 of it.  The output is rounded once, and each probability once
+    before it meets its value.  The cubic adds 2^-10 of one pair in six at most, 0.03 of that in squares."""
+    rows, heads, side, keys = 2, 4, 16, 500
+    g = torch.Generator(device="cuda").manual_seed(D)
+    q, k, v = (torch.randn(rows, heads, n, D, generator=g, device="cuda").bfloat16() for n in (side * side, keys, keys))
+    scale = spread / math.sqrt(D)
+    with Cache(1, heads, D, rows, (side,), [(0, 1, False)], softmax_scale=scale) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+        out = torch.full_like(q, float("nan"))
+        B.amskv_cross_attend(c.h, 0, heads, keys, k, v, q, out)
+        assert B.amskv_status(c.h) == 0
+    p = torch.softmax(scale * (q.double() @ k.double().transpose(2, 3)), -1)
+    want, spread_of_p = p @ v.double(), (p * p) @ (v.double() * v.double())
+    rms = float((out.double() - want).square().mean().sqrt())
+    assert rms <= 2.0 ** -9 * float((want.square() + spread_of_p).mean().sqrt()), rms

@@ -404,3 +404,27 @@ def test_a_path_of_ones_own_choice_depends_on_the_scale_alone(D, path):
 def test_clusters_that_share_long_keys(rows, heads, D, sides):
     """Forms that only calls of few items under AUTO have."""
     test_a_schedule(rows, heads, D, sides, (0, 1, True), "auto")
+
+
+@pytest.mark.parametrize("path", ["rows", "tiles"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_errors_in_the_mean_are_those_of_two_roundings(D, path):
+    """As for cross attention (0.85 * 2^-9 of the output, and of each probability before it meets its value), over the values the cache
+    holds."""
+    sides, rows, heads = (4, 9, 16), 2, 4
+    g = torch.Generator(device="cuda").manual_seed(D)
+    held, scale = [[], []], 1.0 / math.sqrt(D)
+    with Cache(1, heads, D, rows, sides, [(0, 1, True)], flags=B.FLAG_KV_E4M3) as c:
+        B.amskv_set_attend_path(c.h, PATHS[path])
+        for i, s in enumerate(sides):
+            q, k, v = (torch.randn(rows, heads, s * s, D, generator=g, device="cuda").bfloat16() for _ in range(3))
+            out = torch.full_like(q, float("nan"))
+            B.amskv_append_attend(c.h, 0, i, k, v, q, out)
+            assert B.amskv_status(c.h) == 0
+            for x, to in ((k, held[0]), (v, held[1])):
+                to.append(torch.from_numpy(ref.held_values(_np(x))).cuda())
+    kk, vv = (torch.cat(x, 2) for x in held)
+    p = torch.softmax(scale * (q.double() @ kk.transpose(2, 3)), -1)
+    want, spread_of_p = p @ vv, (p * p) @ (vv * vv)
+    rms = float((out.double() - want).square().mean().sqrt())
+    assert rms <= 2.0 ** -9 * float((want.square() + spread_of_p).mean().sqrt()), rms
