@@ -247,7 +247,7 @@ rotary_any_kernel(const __grid_constant__ RotaryArgs a)
             const int64_t n = a.index ? (int64_t)load_int(a.index + row * a.index_row + t) : a.first + t;
             const bool turned = n >= 0 && n < a.table_rows;   // (a token without a position keeps its channels)
             const float2* cs = a.table + n * cols;
-            __nv_bfloat162 out[4];
+            __align__(16) __nv_bfloat162 out[4];   // (stored as one piece)
             __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(out);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
