@@ -97,6 +97,8 @@ extern "C" {
                               amskv_append_attend makes the two calls it stands for; the densities (amskv_attention_density,
                               amskv_attend_density) and AMSKV_PATH_SIMT are refused with UNSUPPORTED, and so are, at creation,
                               token budgets (they cut scales inside a block), BULK_APPEND and TRANSIENT_LAST_SCALE.
+                              AMSKV_PATH_SMALL is the warp-matrix kernel over codes, AMSKV_PATH_TENSOR and AMSKV_PATH_TENSOR_PAIR
+                              the tensor-memory kernel.
                               amskv_cache_bytes counts the codes of resident tokens, not the powers of two. */
 
 /* amskv_set_attend_path */

@@ -23,7 +23,7 @@
 // the products, 128 channels; with codes no unit by itself (64 channels: special-function unit 46 %, issue slots 44 % busy at 425 keys), but the
 // chain of widening, S, softmax and P V, whose waits for tensor memory lead.  4 096 queries x 10 521 keys x 64
 // heads: 64 channels 910 us (0.73 PFLOP/s of products), 128 channels 1 050 (1.26); from codes 1 040 to 1 270 and 1 250 (0.9 and 1.06).
-// 256 queries x 430 keys: 64 channels, 3 840 heads 179, codes 225; 128 channels, 2 048 heads 143, codes 175.
+// 256 queries x 430 keys: 64 channels, 3 840 heads 176, codes 225; 128 channels, 2 048 heads 141, codes 176.
 // Every wait is bounded: one that gives up records a status code and sets a flag, its role stops, and so do the others at their
 // next wait.  Copies and products still under way are then awaited, and the tensor memory is freed.
 #include <algorithm>
